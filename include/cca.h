@@ -305,6 +305,102 @@ cca_status cca_decode_step_ragged(const cca_config *cfg, const cca_weights *w, c
 cca_status cca_decode_step_static(const cca_config *cfg, const cca_weights *w, const void *x_new,
                                   const cca_decode_state *state, int32_t pos, void *out, void *hip_stream);
 
+/* ---- serving with 4 bits a number ------------------------------------------
+ * Format: a number is stored as e2m1 - a sign (bit 3) and one of 0, 0.5, 1,
+ * 1.5, 2, 3, 4, 6 - two to a byte, the even-numbered one in the low half; 32
+ * neighbours share a scale byte E and stand for e2m1 * 2^(E - 127); E = 255:
+ * all 32 are NaN.  (OCP's microscaling form MXFP4; 4.25 bits a number.)  Every
+ * value is a bf16 number: nothing is rounded between the store and the
+ * products.  Storing: with amax = f * 2^e the largest magnitude of the 32, 1 <=
+ * f < 2, E - 127 = e - 2, or e - 1 where f > 1.75, E held within 2..252; each
+ * number is rounded to the nearest multiple, ties to the even code, at most 6.
+ * (Thus a stored number is off by at most a fifth of its group's amax where
+ * that is 2^-123 or more; smaller amax lose more.)  A group that holds a NaN
+ * or an infinity is stored as E = 255.
+ *
+ * The cache: rows of keys and values as cca_prologue writes them (after norm,
+ * temperature and rotary embedding), each KV head's rows next to one another.
+ * cfg->T is its capacity and must be a multiple of 32, d_h a multiple of 32,
+ * else CCA_ERR_UNSUPPORTED.  Of cfg the calls below read B, T, n_q_heads,
+ * n_kv_heads, head_dim, dtype (of k, v, q, o) and softmax_scale; all of it is
+ * validated.  A row carries its rotary angle, so attention does not depend on
+ * where a row lies, and rows of different heads need not be those of the same
+ * tokens.
+ * Lengths, rows and positions are DEVICE arrays of B int32 (4-byte aligned),
+ * read by the kernels of the call only; values outside their range are clamped
+ * on the device, so that no content of an array can carry an access outside
+ * the cache. */
+typedef struct {
+  void *k_codes, *v_codes;   /* (B, H_k, T, d_h/2) */
+  void *k_scales, *v_scales; /* (B, H_k, d_h/32, T) */
+  int32_t *pos;              /* (B, H_k, T) position of each row's token; may be NULL where not needed */
+  float *weight;             /* (B, H_k, T) accumulated attention weight of each row; may be NULL where not needed */
+} cca_mx_cache;
+
+/* A projection's weight W (K, N) in 4 bits: the 32 numbers of a group are
+ * neighbours along K. */
+typedef struct {
+  const void *codes;  /* (N, K/2) */
+  const void *scales; /* (N, K/32) */
+} cca_mx_weight;
+
+/* Bytes of device workspace that suffice for each of cca_decode_attention_mx, cca_cache_evict_mx and (with its latent
+ * ring, whose depth P cca_decode_workspace_size reports) cca_decode_step_mx under cfg. */
+cca_status cca_mx_workspace_size(const cca_config *cfg, size_t *bytes);
+
+/* codes, scales <- w (K, N) of type dtype (row-major, as cca_weights holds it); K a multiple of 32, K and N at most
+ * 65536 (CCA_ERR_SHAPE). */
+cca_status cca_mx_quantize(const void *w, int32_t K, int32_t N, int32_t dtype, void *codes, void *scales, void *hip_stream);
+
+/* y (M, N) = x (M, K) W; x and y of type dtype, sums in fp32, any M >= 1 and N >= 1 up to 65536 each.  The 4-bit form of
+ * cca_down_project / cca_up_project, meant for the few rows of a decode step. */
+cca_status cca_project_mx(const void *x, const cca_mx_weight *w, void *y, int32_t M, int32_t K, int32_t N, int32_t dtype,
+                          void *hip_stream);
+
+/* Stores rows: k, v (B, n, H_k, d_h), 1 <= n <= T.  Entry i of sequence b becomes row rows[b] + i of every head, for i <
+ * counts[b] (NULL: n), as far as the capacity goes; the other entries are not read and no other row is written.  With
+ * cache->pos the row's position becomes pos[b] + i (pos NULL: the row's number), with cache->weight its weight 0. */
+cca_status cca_cache_append_mx(const cca_config *cfg, const cca_mx_cache *cache, const void *k, const void *v, int32_t n,
+                               const int32_t *rows, const int32_t *counts, const int32_t *pos, void *hip_stream);
+
+/* Reads rows back: entry i of sequence b of k, v (B, n, H_k, d_h) is row first[b] + i (NULL: i) for i < counts[b] (NULL: n)
+ * as far as the capacity goes, and zero beyond. */
+cca_status cca_cache_rows_mx(const cca_config *cfg, const cca_mx_cache *cache, void *k, void *v, int32_t n,
+                             const int32_t *first, const int32_t *counts, void *hip_stream);
+
+/* Attention of one new token per sequence: o (B, H_q*d_h) = softmax(scale * q K^T) V over rows 0..len[b]-1 of the cache, q
+ * (B, H_q, d_h), query head h reading KV head h / R.  len[b] is clamped to [0, max_len], 0 <= max_len <= T (CCA_ERR_SHAPE).
+ * A sequence of length 0 gives o = 0.  lse (B, H_q) fp32 may be NULL: the natural logarithm of the sum of exponentials, -inf
+ * for length 0.  weight_out (B, H_k, T) fp32 may be NULL: for each row below len[b] the attention probabilities of the
+ * R query heads are added to weight_in (NULL: to 0; weight_out itself: in place; any other overlap is
+ * CCA_ERR_UNSUPPORTED); rows from len[b] on are left as they were.  Probabilities enter the product with V with 16 bits or more of mantissa. */
+cca_status cca_decode_attention_mx(const cca_config *cfg, const cca_mx_cache *cache, const void *q, const int32_t *len,
+                                   int32_t max_len, void *o, float *lse, const float *weight_in, float *weight_out,
+                                   void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Keeps at most `budget` rows of every head, 1 <= budget <= T, 0 <= recent <= budget (CCA_ERR_SHAPE).  Of the n = len[b]
+ * rows of a (sequence, head) with n > budget stay the `budget` of highest rank: first the rows whose position exceeds the head's
+ * largest one less `recent`, then by weight, the greater first (a NaN last), and of equal ones the lower row.  The kept rows that lie
+ * at or beyond `budget` move, in order, into the places of the rows that went, in order; every other kept row
+ * stays where it is, so that rows 0..budget-1 are the cache afterwards, in no order of position.  What lies beyond is undefined.
+ * Needs cache->pos and cache->weight.  pos_out, weight_out (B, H_k, T) and len_out (B) get the new positions, weights and lengths
+ * min(len[b], budget); NULL or the input itself: in place.  Apart from their input (any other overlap is CCA_ERR_UNSUPPORTED) their entries from
+ * the new length on are left as they were and the input is only read. */
+cca_status cca_cache_evict_mx(const cca_config *cfg, const cca_mx_cache *cache, int32_t *len, int32_t max_len, int32_t budget,
+                              int32_t recent, float *weight_out, int32_t *pos_out, int32_t *len_out, void *workspace,
+                              size_t workspace_bytes, void *hip_stream);
+
+/* cca_decode_step_ragged over a 4-bit cache and 4-bit projections.  Sequence b's new token stands at position pos[b] of its
+ * text (rotary angle, ring slot; clamped to [0, 2^30]) and becomes row len[b] of every head (clamped to [0, max_len], 0 <= max_len < T, else
+ * CCA_ERR_SHAPE): with rows evicted, len[b] is below pos[b].  Its keys and values are stored as cca_cache_append_mx stores them, then
+ * it attends to rows 0..len[b], its own included, as read back.  With cache->weight every row's weight grows by the attention it got, the new row's from
+ * 0; with cache->pos the new row's position is recorded.  pos and len are not advanced.  w_down (E, N_lat) and w_out (e_q, E) are the
+ * weights of cca_weights in 4 bits (E and e_q multiples of 32); of `w` the members w_conv_seq, w_conv_ch and temp are
+ * read.  lat_ring: as in cca_decode_state. */
+cca_status cca_decode_step_mx(const cca_config *cfg, const cca_weights *w, const cca_mx_weight *w_down, const cca_mx_weight *w_out,
+                              const void *x_new, const cca_mx_cache *cache, void *lat_ring, const int32_t *pos, const int32_t *len,
+                              int32_t max_len, void *out, void *workspace, size_t workspace_bytes, void *hip_stream);
+
 /* Measurement aid (not a step of the method): enqueues a kernel of `blocks`
  * workgroups x 4 wavefronts that issue iters x 4 independent 32x32x16 bf16
  * matrix-core instructions each and nothing else, and stores the number of

@@ -30,7 +30,9 @@ CCA_FLAGS_MHA = CCA_CAUSAL
 EXPORTS = ("cca_workspace_size", "cca_backward_workspace_size", "cca_prepared_size", "cca_prepare", "cca_forward",
            "cca_backward", "cca_down_project",
            "cca_prologue", "cca_attention", "cca_attention_backward", "cca_prologue_backward", "cca_up_project",
-           "cca_decode_workspace_size", "cca_decode_step", "cca_decode_step_ragged", "cca_decode_step_static", "cca_probe_mfma_rate", "cca_strerror", "cca_version")
+           "cca_decode_workspace_size", "cca_decode_step", "cca_decode_step_ragged", "cca_decode_step_static", "cca_probe_mfma_rate", "cca_strerror", "cca_version",
+           "cca_mx_workspace_size", "cca_mx_quantize", "cca_project_mx", "cca_cache_append_mx", "cca_cache_rows_mx",
+           "cca_decode_attention_mx", "cca_cache_evict_mx", "cca_decode_step_mx")
 
 
 class cca_config(C.Structure):
@@ -58,6 +60,15 @@ class cca_saved(C.Structure):
 class cca_grads(C.Structure):
     _fields_ = [("w_down", C.c_void_p), ("w_conv_seq", C.c_void_p), ("w_conv_ch", C.c_void_p),
                 ("temp", C.c_void_p), ("w_out", C.c_void_p)]
+
+
+class cca_mx_cache(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p),
+                ("pos", C.c_void_p), ("weight", C.c_void_p)]
+
+
+class cca_mx_weight(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p)]
 
 
 class CCAError(RuntimeError):
@@ -101,6 +112,15 @@ def load_library() -> C.CDLL:
     lib.cca_decode_step_static.argtypes = [cfgp, C.POINTER(cca_weights), vp, C.POINTER(cca_decode_state), C.c_int32, vp,
                                            vp]
     lib.cca_probe_mfma_rate.argtypes = [vp, sz, C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_double), vp]
+    i32, mxc, mxw = C.c_int32, C.POINTER(cca_mx_cache), C.POINTER(cca_mx_weight)
+    lib.cca_mx_workspace_size.argtypes = [cfgp, C.POINTER(sz)]
+    lib.cca_mx_quantize.argtypes = [vp, i32, i32, i32, vp, vp, vp]
+    lib.cca_project_mx.argtypes = [vp, mxw, vp, i32, i32, i32, i32, vp]
+    lib.cca_cache_append_mx.argtypes = [cfgp, mxc, vp, vp, i32, vp, vp, vp, vp]
+    lib.cca_cache_rows_mx.argtypes = [cfgp, mxc, vp, vp, i32, vp, vp, vp]
+    lib.cca_decode_attention_mx.argtypes = [cfgp, mxc, vp, vp, i32, vp, vp, vp, vp, vp, sz, vp]
+    lib.cca_cache_evict_mx.argtypes = [cfgp, mxc, vp, i32, i32, i32, vp, vp, vp, vp, sz, vp]
+    lib.cca_decode_step_mx.argtypes = [cfgp, C.POINTER(cca_weights), mxw, mxw, vp, mxc, vp, vp, vp, i32, vp, vp, sz, vp]
     for name in EXPORTS:
         getattr(lib, name).restype = C.c_int
     lib.cca_strerror.argtypes = [C.c_int]
@@ -469,6 +489,232 @@ def cca_decode_step_static(cfg: CCAConfig, w: CCAWeights, x_new, state: CCADecod
     cc, cw, cs = cfg.c(), w.c(), state.c()
     _check(lib.cca_decode_step_static(C.byref(cc), C.byref(cw), _ptr(x_new), C.byref(cs), C.c_int32(pos), _ptr(out),
                                       _stream()), "cca_decode_step_static")
+    return out
+
+
+# ---- serving with 4 bits a number (format and layouts: cca.h) --------------
+def _mx_arg(name, t, shape, dtype, device):
+    """Address of `t` after the checks that the library cannot make."""
+    if t.device != device:
+        raise ValueError(f"{name}: on {t.device}, expected {device}")
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, expected {dtype} {tuple(shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: libcca takes contiguous tensors")
+    return t.data_ptr()
+
+
+def _mx_rows_arg(name, t, cfg, device):
+    return None if t is None else _mx_arg(name, t, (cfg.B,), torch.int32, device)
+
+
+def _mx_call(where, device, *args):
+    """A call on the tensors' device and on that device's current stream."""
+    if device.type != "cuda":
+        raise ValueError(f"{where}: tensors on {device}, expected a GPU")
+    fn = getattr(load_library(), where)
+    if device.index == torch.cuda.current_device():
+        _check(fn(*args, torch.cuda.current_stream().cuda_stream), where)
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args, torch.cuda.current_stream().cuda_stream), where)
+
+
+@dataclass(frozen=True)
+class CCAMXWeight:
+    """A projection's weight W (K, N) in 4 bits: codes (N, K/2) and scales (N, K/32), uint8 (see cca_mx_weight in cca.h)."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+
+    def __post_init__(self):
+        n, k = self.codes.shape[0], 2 * self.codes.shape[1]
+        _mx_arg("codes", self.codes, (n, k // 2), torch.uint8, self.codes.device)
+        _mx_arg("scales", self.scales, (n, k // 32), torch.uint8, self.codes.device)
+        object.__setattr__(self, "_c", cca_mx_weight(self.codes.data_ptr(), self.scales.data_ptr()))
+
+    @property
+    def K(self):
+        return 2 * self.codes.shape[1]
+
+    @property
+    def N(self):
+        return self.codes.shape[0]
+
+
+@dataclass(frozen=True)
+class CCAMXCache:
+    """Latent keys and values in 4 bits (see cca_mx_cache in cca.h): codes (B, H_k, T, d_h/2) and scales (B, H_k, d_h/32, T), uint8;
+    optionally each row's position (int32) and accumulated attention weight (fp32), (B, H_k, T)."""
+    k_codes: torch.Tensor
+    k_scales: torch.Tensor
+    v_codes: torch.Tensor
+    v_scales: torch.Tensor
+    pos: torch.Tensor | None = None
+    weight: torch.Tensor | None = None
+
+    def __post_init__(self):
+        if self.k_codes.dim() != 4:
+            raise ValueError(f"k_codes: {tuple(self.k_codes.shape)}, expected (B, H_k, T, d_h/2)")
+        B, Hk, T, half = self.k_codes.shape
+        dev, ptrs = self.k_codes.device, {}
+        for name, shape, dt in (("k_codes", (B, Hk, T, half), torch.uint8), ("v_codes", (B, Hk, T, half), torch.uint8),
+                                ("k_scales", (B, Hk, half // 16, T), torch.uint8), ("v_scales", (B, Hk, half // 16, T), torch.uint8),
+                                ("pos", (B, Hk, T), torch.int32), ("weight", (B, Hk, T), torch.float32)):
+            t = getattr(self, name)
+            ptrs[name] = None if t is None else _mx_arg(name, t, shape, dt, dev)
+        object.__setattr__(self, "_c", cca_mx_cache(**ptrs))
+        object.__setattr__(self, "_layout", (B, Hk, T, 2 * half))
+
+    @staticmethod
+    def allocate(cfg: CCAConfig, device, with_weights: bool = True) -> "CCAMXCache":
+        B, Hk, T, dh = cfg.B, cfg.n_kv_heads, cfg.T, cfg.head_dim
+        z = lambda *shape, dtype=torch.uint8: torch.zeros(*shape, dtype=dtype, device=device)
+        return CCAMXCache(z(B, Hk, T, dh // 2), z(B, Hk, dh // 32, T), z(B, Hk, T, dh // 2), z(B, Hk, dh // 32, T),
+                          z(B, Hk, T, dtype=torch.int32) if with_weights else None,
+                          z(B, Hk, T, dtype=torch.float32) if with_weights else None)
+
+    def _for(self, cfg: CCAConfig):
+        if self._layout != (cfg.B, cfg.n_kv_heads, cfg.T, cfg.head_dim):
+            raise ValueError(f"cache of (B, H_k, T, d_h) = {self._layout}, config of {(cfg.B, cfg.n_kv_heads, cfg.T, cfg.head_dim)}")
+        return C.byref(self._c)
+
+
+def cca_mx_workspace_size(cfg: CCAConfig) -> int:
+    n = C.c_size_t(0)
+    cc = cfg.c()
+    _check(load_library().cca_mx_workspace_size(C.byref(cc), C.byref(n)), "cca_mx_workspace_size")
+    return n.value
+
+
+def new_mx_workspace(cfg: CCAConfig, device) -> torch.Tensor:
+    return torch.empty(max(cca_mx_workspace_size(cfg), 256), dtype=torch.uint8, device=device)
+
+
+def cca_mx_quantize(w: torch.Tensor) -> CCAMXWeight:
+    """W (K, N), bf16 or fp32, as CCAWeights holds w_down and w_out, in 4 bits."""
+    if w.dim() != 2 or w.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"cca_mx_quantize: {w.dtype} {tuple(w.shape)}, expected a bf16 or fp32 matrix")
+    K, N = w.shape
+    q = CCAMXWeight(torch.empty(N, K // 2, dtype=torch.uint8, device=w.device), torch.empty(N, K // 32, dtype=torch.uint8, device=w.device))
+    _mx_call("cca_mx_quantize", w.device, _ptr(w), K, N, CCA_BF16 if w.dtype == torch.bfloat16 else CCA_F32, q.codes.data_ptr(),
+             q.scales.data_ptr())
+    return q
+
+
+def cca_project_mx(x: torch.Tensor, w: CCAMXWeight, out: torch.Tensor | None = None) -> torch.Tensor:
+    """x (..., K) W -> (..., N), in x's type (bf16 or fp32)."""
+    K, N, dev = w.K, w.N, w.codes.device
+    if x.dtype not in (torch.bfloat16, torch.float32) or x.dim() < 1 or x.shape[-1] != K:
+        raise ValueError(f"cca_project_mx: x {x.dtype} {tuple(x.shape)}, weight of K = {K}")
+    if out is None:
+        out = torch.empty(*x.shape[:-1], N, dtype=x.dtype, device=dev)
+    _mx_call("cca_project_mx", dev, _mx_arg("x", x, x.shape, x.dtype, dev), C.byref(w._c),
+             _mx_arg("out", out, (*x.shape[:-1], N), x.dtype, dev), x.numel() // K, K, N, CCA_BF16 if x.dtype == torch.bfloat16 else CCA_F32)
+    return out
+
+
+def cca_cache_append_mx(cfg: CCAConfig, cache: CCAMXCache, k, v, rows, pos=None, counts=None) -> None:
+    """Stores k, v (B, n, H_k, d_h) as rows rows[b] ... of every sequence, the first counts[b] of them (None: all), of tokens at
+    positions pos[b] ... (None: the rows' numbers)."""
+    dev, dt = cache.k_codes.device, cfg.torch_dtype
+    n = k.shape[1] if k.dim() == 4 else 0
+    shape = (cfg.B, n, cfg.n_kv_heads, cfg.head_dim)
+    cc = cfg.c()
+    _mx_call("cca_cache_append_mx", dev, C.byref(cc), cache._for(cfg), _mx_arg("k", k, shape, dt, dev), _mx_arg("v", v, shape, dt, dev), n,
+             _mx_rows_arg("rows", rows, cfg, dev), _mx_rows_arg("counts", counts, cfg, dev), _mx_rows_arg("pos", pos, cfg, dev))
+
+
+def cca_cache_rows_mx(cfg: CCAConfig, cache: CCAMXCache, n: int, first=None, count=None, k=None, v=None):
+    """(k, v), (B, n, H_k, d_h): rows first[b] ... (None: 0 ...) of every sequence, zero from the count[b]-th on (None: none)."""
+    dev, dt = cache.k_codes.device, cfg.torch_dtype
+    shape = (cfg.B, n, cfg.n_kv_heads, cfg.head_dim)
+    k = torch.empty(shape, dtype=dt, device=dev) if k is None else k
+    v = torch.empty(shape, dtype=dt, device=dev) if v is None else v
+    cc = cfg.c()
+    _mx_call("cca_cache_rows_mx", dev, C.byref(cc), cache._for(cfg), _mx_arg("k", k, shape, dt, dev), _mx_arg("v", v, shape, dt, dev), n,
+             _mx_rows_arg("first", first, cfg, dev), _mx_rows_arg("count", count, cfg, dev))
+    return k, v
+
+
+def cca_decode_attention_mx(cfg: CCAConfig, cache: CCAMXCache, q, lens, max_len: int, o=None, lse=None, want_lse=False, weight_in=None,
+                            weight_out=None, workspace=None):
+    """o (B, H_q*d_h): attention of one query per sequence, q (B, H_q, d_h), over the first lens[b] <= max_len rows (int32 device
+    tensor).  With weight_out (B, H_k, T) each of those rows' weight_in (None: 0) plus the attention it got goes there."""
+    dev, dt = cache.k_codes.device, cfg.torch_dtype
+    B, Hq = cfg.B, cfg.n_q_heads
+    if o is None:
+        o = torch.empty(B, cfg.e_q, dtype=dt, device=dev)
+    if lse is None and want_lse:
+        lse = torch.empty(B, Hq, dtype=torch.float32, device=dev)
+    if workspace is None:
+        workspace = new_mx_workspace(cfg, dev)
+    w = (B, cfg.n_kv_heads, cfg.T)
+    cc = cfg.c()
+    _mx_call("cca_decode_attention_mx", dev, C.byref(cc), cache._for(cfg), _mx_arg("q", q, (B, Hq, cfg.head_dim), dt, dev),
+             _mx_rows_arg("lens", lens, cfg, dev), max_len, _mx_arg("o", o, (B, cfg.e_q), dt, dev),
+             None if lse is None else _mx_arg("lse", lse, (B, Hq), torch.float32, dev),
+             None if weight_in is None else _mx_arg("weight_in", weight_in, w, torch.float32, dev),
+             None if weight_out is None else _mx_arg("weight_out", weight_out, w, torch.float32, dev),
+             _mx_arg("workspace", workspace, workspace.shape, torch.uint8, dev), workspace.numel())
+    return (o, lse) if want_lse else o
+
+
+def cca_cache_evict_mx(cfg: CCAConfig, cache: CCAMXCache, lens, max_len: int, budget: int, recent: int = 0, weight_out=None, pos_out=None,
+                       lens_out=None, workspace=None) -> None:
+    """Keeps at most `budget` rows of every head: the tokens of the last `recent` positions, then the rows of greatest weight.  Updates
+    cache.pos, cache.weight and lens in place, or leaves them and writes pos_out, weight_out, lens_out."""
+    dev = cache.k_codes.device
+    if workspace is None:
+        workspace = new_mx_workspace(cfg, dev)
+    w = (cfg.B, cfg.n_kv_heads, cfg.T)
+    cc = cfg.c()
+    _mx_call("cca_cache_evict_mx", dev, C.byref(cc), cache._for(cfg), _mx_rows_arg("lens", lens, cfg, dev), max_len, budget, recent,
+             None if weight_out is None else _mx_arg("weight_out", weight_out, w, torch.float32, dev),
+             None if pos_out is None else _mx_arg("pos_out", pos_out, w, torch.int32, dev), _mx_rows_arg("lens_out", lens_out, cfg, dev),
+             _mx_arg("workspace", workspace, workspace.shape, torch.uint8, dev), workspace.numel())
+
+
+@dataclass
+class CCADecodeStateMX:
+    """Device state of a batch of sequences being decoded with a 4-bit cache: the cache and the ring of latent rows."""
+    cache: CCAMXCache
+    lat_ring: torch.Tensor  # (B, P, N_lat)
+    workspace: torch.Tensor
+
+    @staticmethod
+    def allocate(cfg: CCAConfig, device, with_weights: bool = True) -> "CCADecodeStateMX":
+        _, P_ = cca_decode_workspace_size(cfg)
+        return CCADecodeStateMX(CCAMXCache.allocate(cfg, device, with_weights),
+                                torch.zeros(cfg.B, P_, cfg.n_lat, dtype=cfg.torch_dtype, device=device), new_mx_workspace(cfg, device))
+
+    def load_prefill(self, cfg: CCAConfig, saved: CCASaved, n_tokens: int) -> None:
+        """Stores the first n_tokens of a prefill's saved k, v and takes over the last rows of its lat."""
+        zero = torch.zeros(cfg.B, dtype=torch.int32, device=self.lat_ring.device)
+        cca_cache_append_mx(cfg, self.cache, saved.k[:, :n_tokens].contiguous(), saved.v[:, :n_tokens].contiguous(), zero)
+        P_ = self.lat_ring.shape[1]
+        for s in range(max(0, n_tokens - P_), n_tokens):
+            self.lat_ring[:, s % P_].copy_(saved.lat[:, s])
+
+
+def cca_decode_step_mx(cfg: CCAConfig, w: CCAWeights, w_down: CCAMXWeight, w_out: CCAMXWeight, x_new, state: CCADecodeStateMX, pos, lens,
+                       max_len: int, out=None):
+    """out (B, E) for the new token of each sequence, at position pos[b] of its text; it becomes row lens[b] <= max_len of the cache (both
+    int32 device tensors, not advanced).  Of `w` the convolution filters and the temperatures are read."""
+    dev, dt = state.cache.k_codes.device, cfg.torch_dtype
+    if out is None:
+        out = torch.empty(cfg.B, cfg.d_model, dtype=dt, device=dev)
+    for name, q, k, n in (("w_down", w_down, cfg.d_model, cfg.n_lat), ("w_out", w_out, cfg.e_q, cfg.d_model)):
+        if (q.K, q.N) != (k, n) or q.codes.device != dev:
+            raise ValueError(f"{name}: of (K, N) = {(q.K, q.N)} on {q.codes.device}, expected {(k, n)} on {dev}")
+    ring = (cfg.B, state.lat_ring.shape[1], cfg.n_lat)
+    if ring[1] != cca_decode_workspace_size(cfg)[1]:
+        raise ValueError(f"lat_ring: {ring[1]} rows, expected {cca_decode_workspace_size(cfg)[1]}")
+    x_shape = (cfg.B, cfg.d_model)
+    cc, cw = cfg.c(), w.c()
+    _mx_call("cca_decode_step_mx", dev, C.byref(cc), C.byref(cw), C.byref(w_down._c), C.byref(w_out._c), _mx_arg("x_new", x_new, x_shape, dt, dev),
+             state.cache._for(cfg), _mx_arg("lat_ring", state.lat_ring, ring, dt, dev), _mx_rows_arg("pos", pos, cfg, dev),
+             _mx_rows_arg("lens", lens, cfg, dev), max_len, _mx_arg("out", out, x_shape, dt, dev),
+             _mx_arg("workspace", state.workspace, state.workspace.shape, torch.uint8, dev), state.workspace.numel())
     return out
 
 

@@ -588,6 +588,178 @@ cca_status cca_decode_step_ragged(const cca_config *cfg, const cca_weights *w, c
              : CCA_ERR_LAUNCH;
 }
 
+// ---- 4-bit serving ----
+
+// Argument checks that every call over the 4-bit cache makes first (no HIP call).
+static cca_status mx_dims(const cca_config *cfg, Dims *d) {
+  cca_status st = make_dims(cfg, d);
+  if (st != CCA_OK) return st;
+  if (d->dh % 32 != 0 || d->T % 32 != 0) return CCA_ERR_UNSUPPORTED;
+  if ((long long)d->B * d->Hk > (1ll << 22)) return CCA_ERR_SHAPE;  // workgroups of a launch
+  return CCA_OK;
+}
+static bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+static cca_status mx_cache_check(const cca_mx_cache *c) {
+  if (!c || !c->k_codes || !c->k_scales || !c->v_codes || !c->v_scales) return CCA_ERR_NULL;
+  if (!aligned16(c->k_codes) || !aligned16(c->k_scales) || !aligned16(c->v_codes) || !aligned16(c->v_scales) || !aligned16(c->pos) ||
+      !aligned16(c->weight))
+    return CCA_ERR_ALIGN;
+  return CCA_OK;
+}
+static cca_status mx_weight_check(const cca_mx_weight *w) {
+  if (!w || !w->codes || !w->scales) return CCA_ERR_NULL;
+  return aligned16(w->codes) && aligned16(w->scales) ? CCA_OK : CCA_ERR_ALIGN;
+}
+// `out` is `in` or apart from it
+static bool same_or_apart(const void *out, const void *in, size_t bytes) {
+  return !out || !in || out == in || !overlap(out, bytes, in, bytes);
+}
+
+struct MxStepLayout {
+  size_t lat, q, k, v, o, attn, total;  // byte offsets
+};
+static MxStepLayout mx_step_layout(const Dims &d) {
+  MxStepLayout L;
+  size_t off = 0;
+  auto take = [&](size_t bytes) { size_t o = off; off += align_up(bytes, 256); return o; };
+  L.lat = take(d.bf16 ? (size_t)d.B * d.n_lat * sizeof(float) : 0);  // (fp32: the rows go straight into the ring)
+  L.q = take((size_t)d.B * d.e_q * sizeof(float));
+  L.k = take((size_t)d.B * d.e_kv * d.esize());
+  L.v = take((size_t)d.B * d.e_kv * d.esize());
+  L.o = take((size_t)d.B * d.e_q * d.esize());
+  L.attn = take(mx_attention_scratch_bytes(d));
+  L.total = off;
+  return L;
+}
+
+cca_status cca_mx_workspace_size(const cca_config *cfg, size_t *bytes) {
+  if (!bytes) return CCA_ERR_NULL;
+  Dims d;
+  cca_status st = mx_dims(cfg, &d);
+  if (st != CCA_OK) return st;
+  const size_t step = mx_step_layout(d).total, evict = mx_evict_scratch_bytes(d);
+  *bytes = step > evict ? step : evict;
+  return CCA_OK;
+}
+
+cca_status cca_mx_quantize(const void *w, int32_t K, int32_t N, int32_t dtype, void *codes, void *scales, void *hip_stream) {
+  if (dtype != CCA_BF16 && dtype != CCA_F32) return CCA_ERR_DTYPE;
+  if (K <= 0 || N <= 0 || K > 65536 || N > 65536 || K % 32 != 0) return CCA_ERR_SHAPE;
+  if (!w || !codes || !scales) return CCA_ERR_NULL;
+  if (!aligned16(w) || !aligned16(codes) || !aligned16(scales)) return CCA_ERR_ALIGN;
+  return mx_quantize(dtype == CCA_BF16, w, K, N, codes, scales, (hipStream_t)hip_stream) == hipSuccess ? CCA_OK : CCA_ERR_LAUNCH;
+}
+
+cca_status cca_project_mx(const void *x, const cca_mx_weight *w, void *y, int32_t M, int32_t K, int32_t N, int32_t dtype,
+                          void *hip_stream) {
+  if (dtype != CCA_BF16 && dtype != CCA_F32) return CCA_ERR_DTYPE;
+  if (M <= 0 || K <= 0 || N <= 0 || M > 65536 || K > 65536 || N > 65536 || K % 32 != 0) return CCA_ERR_SHAPE;
+  if (!x || !y) return CCA_ERR_NULL;
+  cca_status st = mx_weight_check(w);
+  if (st != CCA_OK) return st;
+  if (!aligned16(x) || !aligned16(y)) return CCA_ERR_ALIGN;
+  return mx_project(dtype == CCA_BF16, x, *w, y, false, RowDest{N, nullptr, 0, 1}, M, K, N, (hipStream_t)hip_stream) == hipSuccess
+             ? CCA_OK
+             : CCA_ERR_LAUNCH;
+}
+
+cca_status cca_cache_append_mx(const cca_config *cfg, const cca_mx_cache *cache, const void *k, const void *v, int32_t n,
+                               const int32_t *rows, const int32_t *counts, const int32_t *pos, void *hip_stream) {
+  Dims d;
+  cca_status st = mx_dims(cfg, &d);
+  if (st != CCA_OK) return st;
+  if (!k || !v || !rows) return CCA_ERR_NULL;
+  st = mx_cache_check(cache);
+  if (st != CCA_OK) return st;
+  if (n < 1 || n > d.T) return CCA_ERR_SHAPE;
+  if (!aligned16(k) || !aligned16(v) || !aligned4(rows) || !aligned4(counts) || !aligned4(pos)) return CCA_ERR_ALIGN;
+  return mx_store(d, *cache, k, v, n, rows, d.T, counts, pos, (hipStream_t)hip_stream) == hipSuccess ? CCA_OK : CCA_ERR_LAUNCH;
+}
+
+cca_status cca_cache_rows_mx(const cca_config *cfg, const cca_mx_cache *cache, void *k, void *v, int32_t n, const int32_t *first,
+                             const int32_t *counts, void *hip_stream) {
+  Dims d;
+  cca_status st = mx_dims(cfg, &d);
+  if (st != CCA_OK) return st;
+  if (!k || !v) return CCA_ERR_NULL;
+  st = mx_cache_check(cache);
+  if (st != CCA_OK) return st;
+  if (n < 1 || n > d.T) return CCA_ERR_SHAPE;
+  if (!aligned16(k) || !aligned16(v) || !aligned4(first) || !aligned4(counts)) return CCA_ERR_ALIGN;
+  return mx_rows(d, *cache, k, v, n, first, counts, (hipStream_t)hip_stream) == hipSuccess ? CCA_OK : CCA_ERR_LAUNCH;
+}
+
+cca_status cca_decode_attention_mx(const cca_config *cfg, const cca_mx_cache *cache, const void *q, const int32_t *len,
+                                   int32_t max_len, void *o, float *lse, const float *weight_in, float *weight_out,
+                                   void *workspace, size_t workspace_bytes, void *hip_stream) {
+  Dims d;
+  cca_status st = mx_dims(cfg, &d);
+  if (st != CCA_OK) return st;
+  if (!q || !len || !o || (weight_in && !weight_out)) return CCA_ERR_NULL;
+  st = mx_cache_check(cache);
+  if (st != CCA_OK) return st;
+  if (max_len < 0 || max_len > d.T) return CCA_ERR_SHAPE;
+  if (!aligned16(q) || !aligned16(o) || !aligned4(len) || !aligned4(lse) || !aligned16(weight_in) || !aligned16(weight_out) ||
+      !aligned16(workspace))
+    return CCA_ERR_ALIGN;
+  if (!same_or_apart(weight_out, weight_in, (size_t)d.B * d.Hk * d.T * sizeof(float))) return CCA_ERR_UNSUPPORTED;
+  if (!workspace || workspace_bytes < mx_attention_scratch_bytes(d)) return CCA_ERR_WORKSPACE;
+  return mx_attention(d, *cache, q, false, len, max_len, 0, o, lse, weight_in, weight_out, workspace, (hipStream_t)hip_stream) == hipSuccess
+             ? CCA_OK
+             : CCA_ERR_LAUNCH;
+}
+
+cca_status cca_cache_evict_mx(const cca_config *cfg, const cca_mx_cache *cache, int32_t *len, int32_t max_len, int32_t budget,
+                              int32_t recent, float *weight_out, int32_t *pos_out, int32_t *len_out, void *workspace,
+                              size_t workspace_bytes, void *hip_stream) {
+  Dims d;
+  cca_status st = mx_dims(cfg, &d);
+  if (st != CCA_OK) return st;
+  st = mx_cache_check(cache);
+  if (st != CCA_OK) return st;
+  if (!len || !cache->pos || !cache->weight) return CCA_ERR_NULL;
+  if (max_len < 0 || max_len > d.T || budget < 1 || budget > d.T || recent < 0 || recent > budget) return CCA_ERR_SHAPE;
+  if (!aligned4(len) || !aligned4(len_out) || !aligned16(weight_out) || !aligned16(pos_out) || !aligned16(workspace)) return CCA_ERR_ALIGN;
+  const size_t rows = (size_t)d.B * d.Hk * d.T * 4;
+  if (!same_or_apart(weight_out, cache->weight, rows) || !same_or_apart(pos_out, cache->pos, rows) || !same_or_apart(len_out, len, (size_t)d.B * 4))
+    return CCA_ERR_UNSUPPORTED;
+  if (!workspace || workspace_bytes < mx_evict_scratch_bytes(d)) return CCA_ERR_WORKSPACE;
+  return mx_evict(d, *cache, len, max_len, budget, recent, weight_out, pos_out, len_out, workspace, (hipStream_t)hip_stream) == hipSuccess
+             ? CCA_OK
+             : CCA_ERR_LAUNCH;
+}
+
+cca_status cca_decode_step_mx(const cca_config *cfg, const cca_weights *w, const cca_mx_weight *w_down, const cca_mx_weight *w_out,
+                              const void *x_new, const cca_mx_cache *cache, void *lat_ring, const int32_t *pos, const int32_t *len,
+                              int32_t max_len, void *out, void *workspace, size_t workspace_bytes, void *hip_stream) {
+  constexpr int POS_MAX = 1 << 30;
+  Dims d;
+  cca_status st = mx_dims(cfg, &d);
+  if (st != CCA_OK) return st;
+  if (d.E % 32 != 0) return CCA_ERR_UNSUPPORTED;
+  if (!w || !x_new || !lat_ring || !pos || !len || !out) return CCA_ERR_NULL;
+  if ((st = mx_weight_check(w_down)) != CCA_OK || (st = mx_weight_check(w_out)) != CCA_OK) return st;
+  if ((st = mx_cache_check(cache)) != CCA_OK) return st;
+  if ((st = check_prologue_weights(d, w)) != CCA_OK) return st;
+  if (max_len < 0 || max_len >= d.T) return CCA_ERR_SHAPE;
+  if (!aligned16(x_new) || !aligned16(lat_ring) || !aligned16(out) || !aligned16(workspace) || !aligned4(pos) || !aligned4(len))
+    return CCA_ERR_ALIGN;
+  const MxStepLayout L = mx_step_layout(d);
+  if (!workspace || workspace_bytes < L.total) return CCA_ERR_WORKSPACE;
+  unsigned char *ws = static_cast<unsigned char *>(workspace);
+  hipStream_t s = (hipStream_t)hip_stream;
+  float *lat = reinterpret_cast<float *>(ws + L.lat), *q = reinterpret_cast<float *>(ws + L.q);
+  const int P = decode_ring_rows(d);
+  const RowDest rows{d.n_lat, nullptr, 0, 1}, ring{(long long)P * d.n_lat, pos, POS_MAX, P};
+  if (mx_project(d.bf16, x_new, *w_down, d.bf16 ? lat : lat_ring, true, d.bf16 ? rows : ring, d.B, d.E, d.n_lat, s) != hipSuccess ||
+      decode_prologue(d, *w, lat, lat_ring, POS_MAX, pos, q, ws + L.k, ws + L.v, s) != hipSuccess ||
+      mx_store(d, *cache, ws + L.k, ws + L.v, 1, len, max_len, nullptr, pos, s) != hipSuccess ||
+      mx_attention(d, *cache, q, true, len, max_len, 1, ws + L.o, nullptr, cache->weight, cache->weight, ws + L.attn, s) != hipSuccess ||
+      mx_project(d.bf16, ws + L.o, *w_out, out, false, RowDest{d.E, nullptr, 0, 1}, d.B, d.e_q, d.E, s) != hipSuccess)
+    return CCA_ERR_LAUNCH;
+  return CCA_OK;
+}
+
 cca_status cca_probe_mfma_rate(void *out, size_t out_bytes, int32_t blocks, int32_t iters, int32_t operands,
                                double *flops, void *hip_stream) {
   if (!out || !flops) return CCA_ERR_NULL;

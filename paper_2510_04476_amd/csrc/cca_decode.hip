@@ -26,6 +26,7 @@ struct DecArgs {
   uint32_t flags;
   float rope_base, scale, norm_eps;
   const int *pos_seq;  // per-sequence positions (device, B entries) or null: every sequence at `pos`
+  bool one_row;        // the new key and value are the only row of `S` = 1 rows, whatever the position
 };
 
 // Position of sequence b's new token.  With per-sequence positions `pos` is the largest one the host vouched for
@@ -176,7 +177,7 @@ __global__ __launch_bounds__(512) void decode_prologue_kernel(DecArgs a, T *__re
                                                              T *__restrict__ k_cache, T *__restrict__ v_cache) {
   extern __shared__ __attribute__((aligned(16))) float sm[];  // y0[dh][k_ch] | yrot[dh] | cos[dh/2] | sin[dh/2]
   const int b = blockIdx.x, head = blockIdx.y, dh = a.dh, tid = threadIdx.x, t = seq_pos(a, b);
-  const long long crow = (long long)b * a.S + t;  // cache row of the new token
+  const long long crow = (long long)b * a.S + (a.one_row ? 0 : t);  // cache row of the new token
   T *const slot = hist + ((long long)b * a.P + t % a.P) * a.n_lat;
   // (fp32: the projection wrote the rows into the ring itself)
   const NewRow<T, NP> now{std::is_same<T, float>::value ? reinterpret_cast<const float *>(slot) : part + (long long)b * a.n_lat,
@@ -919,22 +920,6 @@ int panel_rows(int M, int K) {
   return ((K + passes - 1) / passes + 127) / 128 * 128;
 }
 
-// C row m starts at C + m * ldc (the rows of a projection may go straight into a strided destination).  With `row_pos`
-// row m goes to ring slot clamp(row_pos[m], 0, pos_max) % ring of its sequence: C + m * ldc + slot * N.
-struct RowDest {
-  long long ldc;
-  const int *row_pos;
-  int pos_max, ring;
-  __device__ __forceinline__ long long at(int m, int N) const {
-    long long o = m * ldc;
-    if (row_pos) {
-      const int p = row_pos[m];
-      o += (long long)((p < 0 ? 0 : (p > pos_max ? pos_max : p)) % ring) * N;
-    }
-    return o;
-  }
-};
-
 // (a body inlined with restrict arguments: without them the compiler makes the transposing LDS reads of a later pass wait
 // for loads into LDS that they do not touch)
 // COMBINE: A is not in memory yet, its rows are the sums over the splits of the attention (`cmb`, as decode_combine_kernel forms them),
@@ -1199,13 +1184,36 @@ DecLayout layout(const Dims &d) {
 }
 
 template <typename T>
+hipError_t prologue_t(const Dims &d, const cca_weights &w, const DecArgs &a, const float *gpart, int nparts, void *hist, float *q_new, void *k_cache,
+                      void *v_cache, hipStream_t s) {
+  const int kc = (d.flags & CCA_CONV_CH) ? d.k_ch : 1;
+  const int threads = d.dh <= 64 ? 256 : 512, per_lane = (d.dh * kc / 8 + 7) / 8;  // filter chunks per lane of 8
+  const size_t smem = sizeof(float) * ((size_t)kc * d.dh + 2 * d.dh);
+#define CCA_DEC_PRO_NP(CH, LPO, NP)                                                                                       \
+  decode_prologue_kernel<T, CH, LPO, NP><<<dim3(d.B, d.Hq + 2 * d.Hk), threads, smem, s>>>(                                \
+      a, (T *)hist, gpart, nparts, (const T *)w.w_conv_seq, (const T *)w.w_conv_ch, w.temp, q_new, (T *)k_cache, (T *)v_cache)
+#define CCA_DEC_PRO(CH, LPO)                                                                                              \
+  if (std::is_same<T, float>::value || nparts == 1) CCA_DEC_PRO_NP(CH, LPO, 1);                                            \
+  else if (nparts == 2) CCA_DEC_PRO_NP(CH, LPO, (std::is_same<T, float>::value ? 1 : 2));                                  \
+  else if (nparts <= 5) CCA_DEC_PRO_NP(CH, LPO, (std::is_same<T, float>::value ? 1 : 5));                                  \
+  else CCA_DEC_PRO_NP(CH, LPO, (std::is_same<T, float>::value ? 1 : MAX_PARTS))
+  if (per_lane <= 2) { CCA_DEC_PRO(2, 8); }
+  else if (per_lane <= 4) { CCA_DEC_PRO(4, 8); }
+  else if (per_lane <= 8) { CCA_DEC_PRO(8, 8); }
+  else { CCA_DEC_PRO(8, 16); }
+#undef CCA_DEC_PRO
+#undef CCA_DEC_PRO_NP
+  return hipGetLastError();
+}
+
+template <typename T>
 hipError_t step_t(const Dims &d, const cca_weights &w, const void *x_new, void *k_cache, void *v_cache, void *hist,
                   int pos, const int *pos_seq, void *out, unsigned char *ws, hipStream_t s) {
   // pos: the position of every sequence, or with pos_seq (device, one entry per sequence) the largest of them
   const DecLayout L = layout(d);
   const int P = ring_rows(d);
   DecArgs a{d.B, d.T, d.Hq, d.Hk, d.dh, d.R, d.e_q, d.e_kv, d.n_lat, d.v_half, d.k_seq, d.k_ch, P, pos,
-            d.flags, d.rope_base, d.scale, d.norm_eps, pos_seq};
+            d.flags, d.rope_base, d.scale, d.norm_eps, pos_seq, false};
   float *q_new = reinterpret_cast<float *>(ws + L.q_new);
   T *o = reinterpret_cast<T *>(ws + L.o);
   float *part = reinterpret_cast<float *>(ws + L.part);
@@ -1225,26 +1233,7 @@ hipError_t step_t(const Dims &d, const cca_weights &w, const void *x_new, void *
     e = gemm_skinny<T>((const T *)x_new, (const T *)w.w_down, ring_c, ring, gpart, d.B, d.n_lat, d.E, s);
   }
   if (e != hipSuccess) return e;
-  {
-    const int kc = (d.flags & CCA_CONV_CH) ? d.k_ch : 1;
-    const int threads = d.dh <= 64 ? 256 : 512, per_lane = (d.dh * kc / 8 + 7) / 8;  // filter chunks per lane of 8
-    const size_t smem = sizeof(float) * ((size_t)kc * d.dh + 2 * d.dh);
-#define CCA_DEC_PRO_NP(CH, LPO, NP)                                                                                       \
-  decode_prologue_kernel<T, CH, LPO, NP><<<dim3(d.B, d.Hq + 2 * d.Hk), threads, smem, s>>>(                                \
-      a, (T *)hist, gpart, nparts, (const T *)w.w_conv_seq, (const T *)w.w_conv_ch, w.temp, q_new, (T *)k_cache, (T *)v_cache)
-#define CCA_DEC_PRO(CH, LPO)                                                                                              \
-  if (std::is_same<T, float>::value || nparts == 1) CCA_DEC_PRO_NP(CH, LPO, 1);                                            \
-  else if (nparts == 2) CCA_DEC_PRO_NP(CH, LPO, (std::is_same<T, float>::value ? 1 : 2));                                  \
-  else if (nparts <= 5) CCA_DEC_PRO_NP(CH, LPO, (std::is_same<T, float>::value ? 1 : 5));                                  \
-  else CCA_DEC_PRO_NP(CH, LPO, (std::is_same<T, float>::value ? 1 : MAX_PARTS))
-    if (per_lane <= 2) { CCA_DEC_PRO(2, 8); }
-    else if (per_lane <= 4) { CCA_DEC_PRO(4, 8); }
-    else if (per_lane <= 8) { CCA_DEC_PRO(8, 8); }
-    else { CCA_DEC_PRO(8, 16); }
-#undef CCA_DEC_PRO
-#undef CCA_DEC_PRO_NP
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
+  if ((e = prologue_t<T>(d, w, a, gpart, nparts, hist, q_new, k_cache, v_cache, s)) != hipSuccess) return e;
   {
     const int len = pos + 1;  // the longest sequence sizes the splits
     // (the row kernel addresses a sequence's cache with 32-bit byte offsets)
@@ -1315,6 +1304,13 @@ hipError_t decode_step(const Dims &d, const cca_weights &w, const void *x_new, v
   unsigned char *ws = static_cast<unsigned char *>(workspace);
   return d.bf16 ? step_t<bf16_t>(d, w, x_new, k_cache, v_cache, hist, pos, pos_seq, out, ws, s)
                 : step_t<float>(d, w, x_new, k_cache, v_cache, hist, pos, pos_seq, out, ws, s);
+}
+
+hipError_t decode_prologue(const Dims &d, const cca_weights &w, const float *lat, void *hist, int pos, const int *pos_seq, float *q, void *k,
+                           void *v, hipStream_t s) {
+  const DecArgs a{d.B, 1, d.Hq, d.Hk, d.dh, d.R, d.e_q, d.e_kv, d.n_lat, d.v_half, d.k_seq, d.k_ch, ring_rows(d), pos,
+                  d.flags, d.rope_base, d.scale, d.norm_eps, pos_seq, true};
+  return d.bf16 ? prologue_t<bf16_t>(d, w, a, lat, 1, hist, q, k, v, s) : prologue_t<float>(d, w, a, lat, 1, hist, q, k, v, s);
 }
 
 }  // namespace cca

@@ -199,6 +199,22 @@ hipError_t prologue_fused_prepare(const Dims &d, const cca_weights &w, void *scr
 hipError_t prologue_fused_run(const Dims &d, const cca_weights &w, const void *lat, void *q, void *k, void *v,
                               float *rnorm, const void *scratch, hipStream_t s);
 
+// C row m starts at C + m * ldc (the rows of a projection may go straight into a strided destination).  With `row_pos`
+// row m goes to ring slot clamp(row_pos[m], 0, pos_max) % ring of its sequence: C + m * ldc + slot * N.
+struct RowDest {
+  long long ldc;
+  const int *row_pos;
+  int pos_max, ring;
+  __device__ __forceinline__ long long at(int m, int N) const {
+    long long o = m * ldc;
+    if (row_pos) {
+      const int p = row_pos[m];
+      o += (long long)((p < 0 ? 0 : (p > pos_max ? pos_max : p)) % ring) * N;
+    }
+    return o;
+  }
+};
+
 // ---- decode step (one new token per sequence against the latent KV cache) ----
 int decode_ring_rows(const Dims &d);            // latent rows of history the transforms need: max(taps - 1, 1)
 size_t decode_scratch_bytes(const Dims &d);
@@ -206,5 +222,26 @@ size_t decode_scratch_bytes(const Dims &d);
 // sequence takes its own (clamped to [0, pos] in the kernels)
 hipError_t decode_step(const Dims &d, const cca_weights &w, const void *x_new, void *k_cache, void *v_cache, void *hist,
                        int pos, const int *pos_seq, void *out, void *workspace, hipStream_t s);
+// The transforms of the new token alone: from the fp32 rows of the down-projection (`lat`, (B, N_lat); fp32 storage: the rows are in the
+// ring already) to q (fp32 of the storage type's values, (B, H_q, d_h)) and k, v (B, H_k, d_h); the ring gets the new rows.
+hipError_t decode_prologue(const Dims &d, const cca_weights &w, const float *lat, void *hist, int pos, const int *pos_seq, float *q, void *k,
+                           void *v, hipStream_t s);
+
+// ---- 4-bit serving (include/cca.h) --------------------------------------------
+// bf16: of x and (unless y_f32) y; else both are fp32
+hipError_t mx_project(bool bf16, const void *x, const cca_mx_weight &w, void *y, bool y_f32, const RowDest &dest, int M, int K, int N,
+                      hipStream_t s);
+hipError_t mx_quantize(bool bf16, const void *w, int K, int N, void *codes, void *scales, hipStream_t s);
+// rows[b] is clamped to [0, max_row]
+hipError_t mx_store(const Dims &d, const cca_mx_cache &c, const void *k, const void *v, int n, const int *rows, int max_row,
+                    const int *counts, const int *pos, hipStream_t s);
+hipError_t mx_rows(const Dims &d, const cca_mx_cache &c, void *k, void *v, int n, const int *first, const int *counts, hipStream_t s);
+size_t mx_evict_scratch_bytes(const Dims &d);
+hipError_t mx_evict(const Dims &d, const cca_mx_cache &c, int *len, int max_len, int budget, int recent, float *weight_out, int *pos_out,
+                    int *len_out, void *workspace, hipStream_t s);
+size_t mx_attention_scratch_bytes(const Dims &d);
+// `extra` rows are there beyond each len[b] (the step's new row: its weight starts from 0)
+hipError_t mx_attention(const Dims &d, const cca_mx_cache &c, const void *q, bool q_f32, const int *len, int max_len, int extra, void *o,
+                        float *lse, const float *weight_in, float *weight_out, void *workspace, hipStream_t s);
 
 }  // namespace cca

@@ -1,0 +1,105 @@
+// Device code shared by the 4-bit kernels (cca_mx_cache.hip, cca_mx_attention.hip, cca_mx_project.hip).  The format is that of
+// include/cca.h: e2m1 elements, 32 neighbours to a power-of-two scale byte E, which an instruction takes as the exponent bits of
+// an fp32 number (E << 23; it ignores the sign and the mantissa, and gives NaN for E = 255).  A converted element is a bf16 number
+// exactly.
+#pragma once
+
+#include "cca_internal.h"
+
+namespace cca {
+
+typedef __bf16 mx_bf2 __attribute__((ext_vector_type(2)));
+typedef __bf16 mx_bf8 __attribute__((ext_vector_type(8)));
+typedef uint32_t mx_u2 __attribute__((ext_vector_type(2)));
+typedef uint32_t mx_u3 __attribute__((ext_vector_type(3)));
+typedef uint32_t mx_u4 __attribute__((ext_vector_type(4)));
+typedef float mx_f2 __attribute__((ext_vector_type(2)));
+typedef float mx_f4 __attribute__((ext_vector_type(4)));
+
+// Elements 2 * SEL and 2 * SEL + 1 of eight in `codes`, as a pair of bf16; `scale`: E in bits 23 ... 30
+template <int SEL>
+__device__ __forceinline__ uint32_t mx_pair(uint32_t codes, uint32_t scale) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, __uint_as_float(scale), SEL));
+#else
+  return 0;
+#endif
+}
+// All eight elements of `codes`: an operand of a 16 x 16 x 32 matrix instruction
+__device__ __forceinline__ mx_bf8 mx_eight(uint32_t codes, uint32_t scale) {
+  const mx_u4 r = {mx_pair<0>(codes, scale), mx_pair<1>(codes, scale), mx_pair<2>(codes, scale), mx_pair<3>(codes, scale)};
+  return __builtin_bit_cast(mx_bf8, r);
+}
+// Byte B of a word of scale bytes, moved to bits 23 ... 30 (what lies in the other bits is ignored)
+template <int B>
+__device__ __forceinline__ uint32_t mx_scale_byte(uint32_t bytes) {
+  return B == 3 ? bytes >> 1 : bytes << (23 - 8 * B);
+}
+// Two fp32 numbers rounded to bf16 (nearest, ties to even), packed
+__device__ __forceinline__ uint32_t mx_pack(float lo, float hi) {
+  const mx_bf2 v = {(__bf16)lo, (__bf16)hi};
+  return __builtin_bit_cast(uint32_t, v);
+}
+__device__ __forceinline__ float mx_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float mx_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+__device__ __forceinline__ mx_f4 mx_mfma(mx_bf8 a, mx_bf8 b, mx_f4 c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+#else
+  return c;
+#endif
+}
+
+// The scale byte of a group with largest magnitude `amax` (include/cca.h): floor(log2 amax) - 2, one more above 1.75 * 2^floor, held
+// within 2 ... 252; 255 where the group holds a NaN or an infinity (amax is then one of them).
+__device__ __forceinline__ uint32_t mx_scale_of(float amax) {
+  const uint32_t u = __float_as_uint(amax) & 0x7fffffffu;
+  if (u >= 0x7f800000u) return 255u;
+  const int e = (int)(u >> 23) - 2 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);
+  return (uint32_t)min(max(e, 2), 252);
+}
+// Eight numbers to a word of codes (nearest, ties to the even code, at most 6); 0 under scale 255
+__device__ __forceinline__ uint32_t mx_codes(const float (&x)[8], uint32_t scale) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const float s = __uint_as_float(scale << 23);
+  uint32_t w = 0;
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], s, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], s, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], s, 2);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], s, 3);
+  return scale == 255u ? 0u : w;
+#else
+  return 0;
+#endif
+}
+// max that keeps a NaN (of magnitudes: the bits order them, NaNs above all)
+__device__ __forceinline__ float mx_max_abs(float a, float b) {
+  return __uint_as_float(max(__float_as_uint(a) & 0x7fffffffu, __float_as_uint(b) & 0x7fffffffu));
+}
+
+template <int CTRL>
+__device__ __forceinline__ float mx_dpp(float x) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xf, 0xf, true));
+}
+// Over lane and lane ^ 32, lane ^ 16
+__device__ __forceinline__ float mx_xor32_add(float x) {
+  const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(w[0]) + __uint_as_float(w[1]);
+}
+__device__ __forceinline__ float mx_xor16_add(float x) {
+  const auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(w[0]) + __uint_as_float(w[1]);
+}
+__device__ __forceinline__ float mx_xor32_max(float x) {
+  const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
+}
+__device__ __forceinline__ float mx_xor16_max(float x) {
+  const auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
+}
+
+__device__ __forceinline__ int mx_clamp(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
+
+}  // namespace cca

@@ -1,0 +1,476 @@
+// Attention of one new token per sequence over the 4-bit latent cache (include/cca.h), and the sums of its probabilities per
+// cached row.
+//
+// With R query heads to a KV head and 17/32 bytes a number, the products (4 R flops a number read) are too many for the vector
+// ALU once the cache comes in at the chip's rate, so both run on the matrix cores (16 x 16 x 32, bf16): the conversion of
+// 4-bit elements to bf16 is exact and takes one instruction for two of them.
+#include <type_traits>
+
+#include "cca_mx.h"
+
+namespace cca {
+
+namespace {
+
+constexpr int WAVES = 4;
+
+struct AttnArgs {
+  int B, T, Hq, Hk, R, max_len, extra, nsplit, per, r0;
+  float c;         // scale * log2(e)
+  const int *len;  // rows of each sequence: clamp(len[b], 0, max_len) + extra
+  const void *q;
+  bool q_f32;  // q holds fp32 (of the storage type's values)
+  const unsigned char *k_codes, *k_scales, *v_codes, *v_scales;
+  float *part;    // (B, H_q, nsplit, 2 + d_h): m, l, o of a split (nsplit > 1)
+  float *scores;  // (B, H_q, T) in log2 units, or null
+  void *o;
+  float *lse;
+};
+
+__device__ __forceinline__ int seq_len(const AttnArgs &a, int b) { return mx_clamp(a.len[b], 0, a.max_len) + a.extra; }
+
+// ---------------------------------------------------------------------------
+// Workgroup = (sequence, KV head, split of its rows), four wavefronts, each a block of 16 NT rows at a time.
+// Lane (m, j) = (lane mod 16, lane / 16).
+//   Scores: S (16 rows x 16 columns) = K (A operand: row m, channels j d_h/4 ...) x q (B operand: column m).  Tile t holds rows NT m + t of
+//     the block, so that lane (m, j) gets the scores of column m at the 4 NT adjacent rows 4 NT j ...
+//   O^T (channels x columns) = V^T (A operand: channel of m; rows of j) x P (B operand: column m; rows of j): a lane's own
+//     probabilities are its operand, nothing is exchanged.  For V^T a lane takes the same 8 (4, 2) channels of 8 rows and
+//     pairs neighbouring rows by byte permutations.  Lane (m, j) ends with 8 PB NP adjacent channels of column m.
+// Columns are query heads; the softmax of a column needs its maximum over the four j only, two lane exchanges per block.
+// TERMS: parts of q and P, so that the products keep their precision.  1: bf16 storage, up to 8 heads: q is exact,
+//   columns 8 ... 15 repeat the heads and take the part of P that rounding dropped (added at the end).  2: up to
+//   16 heads: the two parts of P in two products.  3: fp32 storage: three parts of both.
+// Rows past the end: addresses are clamped into the capacity, scores replaced by -inf, scale bytes by 0 (their contents may be NaN).
+// ---------------------------------------------------------------------------
+template <int N32, int TERMS>
+struct Form {
+  static constexpr int DH = 32 * N32, NT = N32 <= 4 ? 4 : 2, BLK = 16 * NT;
+  static constexpr int PB = N32 == 1 ? 1 : N32 == 2 ? 2 : 4;      // bytes of a row's codes that a lane takes for V^T at once
+  static constexpr int NP = PB < 4 ? 1 : (N32 + 3) / 4;           // pieces, 16 PB bytes apart
+  static constexpr int VT = 2 * PB * NP;                          // tiles of 16 channels
+  static constexpr int NG = N32 == 1 || N32 == 2 || N32 == 4 ? 1 : N32 == 8 ? 2 : (N32 + 2) / 4 + 1;  // groups that a lane's K channels touch
+  static constexpr int COLS = TERMS == 1 ? 8 : 16;                // heads of a pass
+  static constexpr int STRIDE = DH + 4;                           // floats of a head in the merge area: m, l, -, -, o
+};
+
+template <int N32, int TERMS>
+__global__ __launch_bounds__(WAVES * 64) void mx_attn_kernel(AttnArgs a) {
+  typedef Form<N32, TERMS> F;
+  constexpr int DH = F::DH, NT = F::NT, BLK = F::BLK, PB = F::PB, NP = F::NP, VT = F::VT, NG = F::NG;
+  extern __shared__ __attribute__((aligned(16))) float mrg[];  // [WAVES][COLS][STRIDE]
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 15, j = lane >> 4;
+  const int split = blockIdx.x % a.nsplit, g = (blockIdx.x / a.nsplit) % a.Hk, b = blockIdx.x / (a.nsplit * a.Hk);
+  const int nr = min(F::COLS, a.R - a.r0);
+  const int len = seq_len(a, b), k_begin = split * a.per, k_end = min(len, k_begin + a.per);
+  if (k_begin >= len && split > 0) return;  // a short sequence has fewer splits: nobody reads the others' place
+  const long long head = (long long)b * a.Hk + g;
+
+  // q: column m's channels j d_h/4 + 8 s + 0 ... 7, in TERMS parts
+  const int col = TERMS == 1 ? m & 7 : m;
+  const long long hq = (long long)b * a.Hq + g * a.R + a.r0 + min(col, nr - 1);  // columns past the last head repeat it; nobody stores them
+  mx_bf8 qf[N32][TERMS == 3 ? 3 : 1];
+#pragma unroll
+  for (int s = 0; s < N32; ++s) {
+    const long long at = hq * DH + j * (DH / 4) + 8 * s;
+    if (TERMS < 3 && !a.q_f32) {
+      qf[s][0] = __builtin_bit_cast(mx_bf8, *reinterpret_cast<const mx_u4 *>(static_cast<const bf16_t *>(a.q) + at));
+    } else {
+      const mx_f4 x = *reinterpret_cast<const mx_f4 *>(static_cast<const float *>(a.q) + at), y = *reinterpret_cast<const mx_f4 *>(static_cast<const float *>(a.q) + at + 4);
+      float r[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+#pragma unroll
+      for (int u = 0; u < (TERMS == 3 ? 3 : 1); ++u) {
+        mx_u4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          w[i] = mx_pack(r[2 * i], r[2 * i + 1]);
+          const uint32_t wi = w[i];
+          r[2 * i] -= mx_lo(wi), r[2 * i + 1] -= mx_hi(wi);
+        }
+        qf[s][u] = __builtin_bit_cast(mx_bf8, w);
+      }
+    }
+  }
+
+  float mx = -INFINITY, l = 0.f;
+  mx_f4 o[VT];
+#pragma unroll
+  for (int t = 0; t < VT; ++t) o[t] = mx_f4{0.f, 0.f, 0.f, 0.f};
+
+  int k0 = k_begin + wave * BLK;
+  if (k0 < k_end) {  // wave-uniform
+    const unsigned char *const kc = a.k_codes + (head * a.T + k_begin) * (DH / 2) + j * (DH / 8);
+    const unsigned char *const vc = a.v_codes + (head * a.T + k_begin) * (DH / 2) + (PB < 4 ? m * PB : 0);
+    const unsigned char *const ks = a.k_scales + head * N32 * a.T + k_begin, *const vs = a.v_scales + head * N32 * a.T + k_begin;
+    const int rows = a.T - k_begin;  // of this head, from here
+    int g0 = j * N32 / 4;            // first group of the lane's K channels
+    uint32_t kw[NT][N32], vw[NT * 4][NP], sk[NG], sv[NP][NT];
+    int vp[NP], vg[NP];  // offset of a piece in the row; its group
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      const int dw = 16 * p + m;  // (PB = 4) word of the row; those past it repeat the last, nobody stores their channels
+      vp[p] = PB < 4 ? 0 : 4 * min(dw, 4 * N32 - 1);
+      vg[p] = PB == 1 ? 0 : PB == 2 ? m >> 3 : min(dw, 4 * N32 - 1) >> 2;
+    }
+    auto load_k = [&](int kk) __attribute__((always_inline)) {
+      const int row = min(kk - k_begin + NT * m, rows - NT);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) __builtin_memcpy(kw[t], __builtin_assume_aligned(kc + (uint32_t)(row + t) * (uint32_t)(DH / 2), N32 % 4 == 0 ? 16 : 4 * (N32 & -N32)), 4 * N32);
+#pragma unroll
+      for (int i = 0; i < NG; ++i) {
+        const unsigned char *p = ks + (long long)min(g0 + i, N32 - 1) * a.T + row;
+        if constexpr (NT == 4) sk[i] = *reinterpret_cast<const uint32_t *>(p);
+        else sk[i] = *reinterpret_cast<const uint16_t *>(p);
+      }
+    };
+    auto load_v = [&](int kk) __attribute__((always_inline)) {
+      const int row = min(kk - k_begin + 4 * NT * j, rows - 4 * NT);
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        const unsigned char *sp = vs + (long long)vg[p] * a.T + row;
+        if constexpr (NT == 4) {
+          const mx_u4 w = *reinterpret_cast<const mx_u4 *>(sp);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sv[p][i] = w[i];
+        } else {
+          const mx_u2 w = *reinterpret_cast<const mx_u2 *>(sp);
+          sv[p][0] = w[0], sv[p][1] = w[1];
+        }
+#pragma unroll
+        for (int i = 0; i < 4 * NT; ++i) {
+          const unsigned char *cp = vc + (uint32_t)row * (uint32_t)(DH / 2) + vp[p] + i * (DH / 2);
+          if constexpr (PB == 4) vw[i][p] = *reinterpret_cast<const uint32_t *>(cp);
+          else if constexpr (PB == 2) vw[i][p] = *reinterpret_cast<const uint16_t *>(cp);
+          else vw[i][p] = *cp;
+        }
+      }
+    };
+    load_k(k0);
+    __builtin_amdgcn_sched_barrier(0);
+    load_v(k0);
+    __builtin_amdgcn_sched_barrier(0);
+    float *const sc = a.scores ? a.scores + hq * a.T : nullptr;
+
+    auto block = [&](auto last_) __attribute__((always_inline)) {
+      constexpr bool LAST = decltype(last_)::value;
+      mx_f4 s[NT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        s[t] = mx_f4{0.f, 0.f, 0.f, 0.f};
+        uint32_t scale[NG];
+#pragma unroll
+        for (int i = 0; i < NG; ++i) scale[i] = t == 0 ? mx_scale_byte<0>(sk[i]) : t == 1 ? mx_scale_byte<1>(sk[i]) : t == 2 ? mx_scale_byte<2>(sk[i]) : mx_scale_byte<3>(sk[i]);
+#pragma unroll
+        for (int x = 0; x < N32; ++x) {
+          uint32_t sx = scale[0];
+          if constexpr (NG > 1) {
+            if constexpr (N32 == 8) sx = scale[x / 4];
+            else {
+              const int gi = (j * N32 + x) / 4 - g0;
+#pragma unroll
+              for (int i = 1; i < NG; ++i) sx = gi == i ? scale[i] : sx;
+            }
+          }
+          const mx_bf8 kf = mx_eight(kw[t][x], sx);
+#pragma unroll
+          for (int u = 0; u < (TERMS == 3 ? 3 : 1); ++u) s[t] = mx_mfma(kf, qf[x][u], s[t]);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (!LAST) load_k(k0 + WAVES * BLK);
+      __builtin_amdgcn_sched_barrier(0);
+      // rows 4 NT j + NT i + t of the block, i = 0 ... 3
+      const int mine = k0 + 4 * NT * j;
+      float best = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float x = s[t][i] * a.c;
+          if constexpr (LAST) x = mine + NT * i + t < k_end ? x : -INFINITY;
+          s[t][i] = x;
+          best = fmaxf(best, x);
+        }
+      if (sc && col == m && col < nr) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (!LAST || mine + NT * i < k_end) {  // (a score past the end is stored inside the capacity, never read)
+            if constexpr (NT == 4) *reinterpret_cast<mx_f4 *>(sc + mine + 4 * i) = mx_f4{s[0][i], s[1][i], s[NT - 2][i], s[NT - 1][i]};
+            else *reinterpret_cast<mx_f2 *>(sc + mine + 2 * i) = mx_f2{s[0][i], s[1][i]};
+          }
+      }
+      best = mx_xor16_max(mx_xor32_max(best));
+      if (__any(best > mx)) {
+        const float top = fmaxf(mx, best), ref = top == -INFINITY ? 0.f : top;
+        const float alpha = __builtin_amdgcn_exp2f(mx - ref);
+        mx = top;
+        l *= alpha;
+#pragma unroll
+        for (int t = 0; t < VT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[t][i] *= alpha;
+      }
+      const float ref = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[t][i] = __builtin_amdgcn_exp2f(s[t][i] - ref);
+          l += s[t][i];
+        }
+      // scale bytes of rows past the end: any finite scale does, their probability is 0
+      if constexpr (LAST) {
+        const int live = k_end - mine;
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+#pragma unroll
+          for (int w = 0; w < NT; ++w) {
+            const int nb = mx_clamp(live - 4 * w, 0, 4);
+            sv[p][w] &= nb == 4 ? ~0u : (1u << (8 * nb)) - 1u;
+          }
+      }
+      // 32 rows at a time: slots e = 0 ... 7 of lane (m, j) are its rows 8 h + e
+#pragma unroll
+      for (int h = 0; h < NT / 2; ++h) {
+        mx_u4 pf[TERMS];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {  // rows 8 h + 2 x, + 1: tile (row mod NT), i = row / NT
+          const int ra = 8 * h + 2 * x;
+          float pa = s[ra % NT][ra / NT], pb = s[(ra + 1) % NT][(ra + 1) / NT];
+          const uint32_t hi = mx_pack(pa, pb);
+          pa -= mx_lo(hi), pb -= mx_hi(hi);
+          const uint32_t mid = mx_pack(pa, pb);
+          if constexpr (TERMS == 1) {
+            pf[0][x] = m & 8 ? mid : hi;
+          } else {
+            pf[0][x] = hi, pf[1][x] = mid;
+            if constexpr (TERMS == 3) pf[2][x] = mx_pack(pa - mx_lo(mid), pb - mx_hi(mid));
+          }
+        }
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+          uint32_t pair[8][PB];  // row e: channels 2 y, 2 y + 1 of the piece
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int r = 8 * h + e;
+            const uint32_t word = sv[p][r / 4], sb = r % 4 == 0 ? mx_scale_byte<0>(word) : r % 4 == 1 ? mx_scale_byte<1>(word) : r % 4 == 2 ? mx_scale_byte<2>(word) : mx_scale_byte<3>(word);
+            pair[e][0] = mx_pair<0>(vw[r][p], sb);
+            if constexpr (PB > 1) pair[e][1] = mx_pair<1>(vw[r][p], sb);
+            if constexpr (PB > 2) pair[e][2] = mx_pair<2>(vw[r][p], sb), pair[e][3] = mx_pair<3>(vw[r][p], sb);
+          }
+#pragma unroll
+          for (int y = 0; y < 2 * PB; ++y) {
+            mx_u4 vf;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) vf[x] = __builtin_amdgcn_perm(pair[2 * x + 1][y / 2], pair[2 * x][y / 2], y % 2 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+            for (int u = 0; u < TERMS; ++u) o[p * 2 * PB + y] = mx_mfma(__builtin_bit_cast(mx_bf8, vf), __builtin_bit_cast(mx_bf8, pf[u]), o[p * 2 * PB + y]);
+          }
+        }
+      }
+      if constexpr (!LAST) {
+        __builtin_amdgcn_sched_barrier(0);
+        load_v(k0 + WAVES * BLK);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    for (; k0 + WAVES * BLK < k_end; k0 += WAVES * BLK) block(std::false_type{});
+    block(std::true_type{});
+  }
+
+  // Merge.  l: over the four j; with one term the upper columns' share of O comes to the lower ones.
+  l = mx_xor16_add(mx_xor32_add(l));
+  if constexpr (TERMS == 1) {
+#pragma unroll
+    for (int t = 0; t < VT; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[t][i] += mx_dpp<0x128>(o[t][i]);  // row_ror 8: the other half of 16 lanes
+  }
+  if (m < nr && m < F::COLS) {
+    float *dst = mrg + (wave * F::COLS + m) * F::STRIDE;
+    if (j == 0) dst[0] = mx, dst[1] = l;
+    // element (p, y, i) is channel 2 PB (16 p + 4 j + i) + y
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int ch = 2 * PB * (16 * p + 4 * j + i);
+        if (ch < DH) {
+#pragma unroll
+          for (int y = 0; y < 2 * PB; y += 2) *reinterpret_cast<mx_f2 *>(dst + 4 + ch + y) = mx_f2{o[p * 2 * PB + y][i], o[p * 2 * PB + y + 1][i]};
+        }
+      }
+  }
+  __syncthreads();
+  for (int x = tid; x < nr * DH; x += WAVES * 64) {
+    const int r = x / DH, ch = x % DH;
+    float M = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) M = fmaxf(M, mrg[(w * F::COLS + r) * F::STRIDE]);
+    float L = 0.f, acc = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      const float *src = mrg + (w * F::COLS + r) * F::STRIDE;
+      const float f = src[0] == -INFINITY && src[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(src[0] - M);
+      L = fmaf(src[1], f, L);
+      acc = fmaf(src[4 + ch], f, acc);
+    }
+    const long long h = (long long)b * a.Hq + g * a.R + a.r0 + r;
+    if (a.part) {
+      float *out = a.part + (h * a.nsplit + split) * (2 + DH);
+      if (ch == 0) out[0] = M, out[1] = L;
+      out[2 + ch] = acc;
+    } else {
+      const float res = L == 0.f ? 0.f : acc / L;
+      if constexpr (TERMS == 3) static_cast<float *>(a.o)[h * DH + ch] = res;
+      else store_f(static_cast<bf16_t *>(a.o) + h * DH + ch, res);
+      if (ch == 0 && a.lse) a.lse[h] = (M + log2f(L)) * 0.69314718055994530942f;
+    }
+  }
+}
+
+// The splits of a (sequence, query head) joined: o = sum o_s 2^(m_s - M) / sum l_s 2^(m_s - M), in index order.
+template <typename T>
+__global__ __launch_bounds__(256) void mx_combine_kernel(AttnArgs a, int dh) {
+  __shared__ float f[256];
+  __shared__ float red[8];
+  const int tid = threadIdx.x, stride = 2 + dh, lane = tid & 63, wave = tid >> 6;
+  for (long long bh = blockIdx.x; bh < (long long)a.B * a.Hq; bh += gridDim.x, __syncthreads()) {
+    const int len = seq_len(a, (int)(bh / a.Hq)), n = max(1, min(a.nsplit, (len + a.per - 1) / a.per));  // (nsplit <= 256)
+    const float *src = a.part + bh * a.nsplit * stride;
+    const float ms = tid < n ? src[(long long)tid * stride] : -INFINITY, ls = tid < n ? src[(long long)tid * stride + 1] : 0.f;
+    float M = ms;
+    for (int off = 32; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
+    if (lane == 0) red[wave] = M;
+    __syncthreads();
+    M = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    const float w = ms == -INFINITY && ls == 0.f ? 0.f : __builtin_amdgcn_exp2f(ms - M);
+    float L = ls * w;
+    for (int off = 32; off > 0; off >>= 1) L += __shfl_xor(L, off);
+    if (lane == 0) red[4 + wave] = L;
+    f[tid] = w;
+    __syncthreads();
+    L = (red[4] + red[5]) + (red[6] + red[7]);
+    if (tid < dh) {
+      float acc = 0.f;
+      for (int s = 0; s < n; ++s) acc = fmaf(src[(long long)s * stride + 2 + tid], f[s], acc);
+      store_f(static_cast<T *>(a.o) + bh * dh + tid, L == 0.f ? 0.f : acc / L);
+    }
+    if (tid == 0 && a.lse) a.lse[bh] = (M + log2f(L)) * 0.69314718055994530942f;
+  }
+}
+
+// weight_out[row] = weight_in[row] + sum over the R query heads of 2^(score - M) / L, four rows a thread; M and L from the splits' states.
+constexpr int W_ROWS = 1024, W_HEADS = 16;
+__global__ __launch_bounds__(256) void mx_weight_kernel(AttnArgs a, int dh, int tiles, const float *weight_in, float *weight_out, int fresh) {
+  __shared__ float top[W_HEADS], inv[W_HEADS];
+  const int tid = threadIdx.x, stride = 2 + dh, lane = tid & 63, wave = tid >> 6;
+  for (long long tile = blockIdx.x; tile < (long long)a.B * a.Hk * tiles; tile += gridDim.x) {
+  const long long head = tile / tiles;
+  const int b = (int)(head / a.Hk), g = (int)(head % a.Hk), len = seq_len(a, b), row = (int)(tile % tiles) * W_ROWS + 4 * tid;
+  if (row - 4 * tid >= len) continue;
+  const int n = min(a.nsplit, (len + a.per - 1) / a.per);
+  mx_f4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int r0 = 0; r0 < a.R; r0 += W_HEADS) {
+    __syncthreads();
+    for (int r = wave; r < min(W_HEADS, a.R - r0); r += 4) {
+      const float *src = a.part + ((long long)b * a.Hq + g * a.R + r0 + r) * a.nsplit * stride;
+      float M = -INFINITY, L = 0.f;
+      for (int s = lane; s < n; s += 64) M = fmaxf(M, src[(long long)s * stride]);
+      for (int off = 32; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
+      for (int s = lane; s < n; s += 64) {
+        const float ms = src[(long long)s * stride], ls = src[(long long)s * stride + 1];
+        L += ms == -INFINITY && ls == 0.f ? 0.f : ls * __builtin_amdgcn_exp2f(ms - M);
+      }
+      for (int off = 32; off > 0; off >>= 1) L += __shfl_xor(L, off);
+      if (lane == 0) top[r] = M, inv[r] = 1.f / L;
+    }
+    __syncthreads();
+    if (row < len)
+      for (int r = 0; r < min(W_HEADS, a.R - r0); ++r) {
+        const mx_f4 s = *reinterpret_cast<const mx_f4 *>(a.scores + ((long long)b * a.Hq + g * a.R + r0 + r) * a.T + row);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] = fmaf(__builtin_amdgcn_exp2f(s[i] - top[r]), inv[r], sum[i]);
+      }
+  }
+  const long long at = head * a.T + row;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (row + i < len) weight_out[at + i] = (weight_in && row + i < len - fresh ? weight_in[at + i] : 0.f) + sum[i];
+  }
+}
+
+size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+
+template <int N32, int TERMS>
+hipError_t launch(const AttnArgs &a, hipStream_t s) {
+  typedef Form<N32, TERMS> F;
+  constexpr size_t lds = sizeof(float) * WAVES * F::COLS * F::STRIDE;
+  if (hipError_t e = raise_lds_limit<mx_attn_kernel<N32, TERMS>>(lds); e != hipSuccess) return e;
+  mx_attn_kernel<N32, TERMS><<<(unsigned)((long long)a.B * a.Hk * a.nsplit), WAVES * 64, lds, s>>>(a);
+  return hipGetLastError();
+}
+template <int TERMS>
+hipError_t launch_width(int n32, const AttnArgs &a, hipStream_t s) {
+  switch (n32) {
+    case 1: return launch<1, TERMS>(a, s);
+    case 2: return launch<2, TERMS>(a, s);
+    case 3: return launch<3, TERMS>(a, s);
+    case 4: return launch<4, TERMS>(a, s);
+    case 5: return launch<5, TERMS>(a, s);
+    case 6: return launch<6, TERMS>(a, s);
+    case 7: return launch<7, TERMS>(a, s);
+    default: return launch<8, TERMS>(a, s);
+  }
+}
+
+}  // namespace
+
+struct MxAttnLayout {
+  size_t part, scores, total;
+};
+static MxAttnLayout mx_attn_layout(const Dims &d) {
+  MxAttnLayout L;
+  L.part = 0;
+  L.scores = align256((size_t)d.B * d.Hq * mx_max_splits((long long)d.B * d.Hk, d.T) * (2 + d.dh) * sizeof(float));
+  L.total = L.scores + align256((size_t)d.B * d.Hq * d.T * sizeof(float));
+  return L;
+}
+size_t mx_attention_scratch_bytes(const Dims &d) { return mx_attn_layout(d).total; }
+
+hipError_t mx_attention(const Dims &d, const cca_mx_cache &c, const void *q, bool q_f32, const int *len, int max_len, int extra, void *o,
+                        float *lse, const float *weight_in, float *weight_out, void *workspace, hipStream_t s) {
+  const MxAttnLayout L = mx_attn_layout(d);
+  unsigned char *ws = static_cast<unsigned char *>(workspace);
+  const int longest = max_len + extra;
+  const int per = mx_rows_per_split((long long)d.B * d.Hk, d.T, longest, d.dh), nsplit = longest > per ? (longest + per - 1) / per : 1;
+  auto p = [](const void *x) { return static_cast<const unsigned char *>(x); };
+  AttnArgs a{d.B, d.T, d.Hq, d.Hk, d.R, max_len, extra, nsplit, per, 0, d.scale * 1.44269504088896340736f, len, q, q_f32 || !d.bf16,
+             p(c.k_codes), p(c.k_scales), p(c.v_codes), p(c.v_scales),
+             nsplit > 1 || weight_out ? reinterpret_cast<float *>(ws + L.part) : nullptr,
+             weight_out ? reinterpret_cast<float *>(ws + L.scores) : nullptr, o, lse};
+  hipError_t e;
+  for (; a.r0 < d.R;) {
+    const int left = d.R - a.r0;
+    if (!d.bf16) e = launch_width<3>(d.dh / 32, a, s), a.r0 += 16;
+    else if (left <= 8) e = launch_width<1>(d.dh / 32, a, s), a.r0 += 8;
+    else e = launch_width<2>(d.dh / 32, a, s), a.r0 += 16;
+    if (e != hipSuccess) return e;
+  }
+  if (a.part) {
+    const long long heads = (long long)d.B * d.Hq;
+    const unsigned grid = (unsigned)(heads < (1 << 20) ? heads : 1 << 20);
+    if (d.bf16) mx_combine_kernel<bf16_t><<<grid, 256, 0, s>>>(a, d.dh);
+    else mx_combine_kernel<float><<<grid, 256, 0, s>>>(a, d.dh);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  if (weight_out && longest > 0) {
+    const int tiles = (longest + W_ROWS - 1) / W_ROWS;
+    const long long all = (long long)d.B * d.Hk * tiles;
+    mx_weight_kernel<<<(unsigned)(all < (1 << 20) ? all : 1 << 20), 256, 0, s>>>(a, d.dh, tiles, weight_in, weight_out, extra);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace cca

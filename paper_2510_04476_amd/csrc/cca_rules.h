@@ -461,4 +461,18 @@ inline bool decode_up_combines(long long B, int e_q, int nsplit, int max_splits)
 constexpr size_t decode_up_lds(long long B, int e_q) { return (size_t)((e_q + 127) / 128 * 128) * (size_t)(64 + 2 * B); }
 constexpr size_t DECODE_UP_LDS = decode_up_lds(1, UP_CHANNELS);
 
+// ---- attention over the 4-bit cache: rows of a split ----------------------------------------------------------------------
+// Every split but a sequence's last holds this many rows: whole rounds of the kernel's four wavefronts (64 rows each, 32 above d_h =
+// 128), as few splits as leave about 1024 workgroups on the chip.  groups = sequences x KV heads.
+constexpr int MX_MAX_SPLITS = 256;
+inline int mx_max_splits(long long groups, int T) {
+  const long long want = groups < 1024 ? 1024 / groups : 1, rounds = (T + 127) / 128;
+  const long long s = want < rounds ? want : rounds;
+  return (int)(s < MX_MAX_SPLITS ? s : MX_MAX_SPLITS);
+}
+inline int mx_rows_per_split(long long groups, int T, int longest, int dh) {
+  const int unit = dh <= 128 ? 256 : 128, most = mx_max_splits(groups, T), even = (longest + most - 1) / most;
+  return even <= unit ? unit : (even + unit - 1) / unit * unit;
+}
+
 }  // namespace cca

@@ -1,0 +1,28 @@
+"""The dispatch rules of the 4-bit attention (csrc/cca_rules.h), compiled for the host."""
+import ctypes as C
+import os
+import subprocess
+import tempfile
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+SOURCE = r"""
+#include "cca_rules.h"
+extern "C" {
+int r_max_splits(long long groups, int T) { return cca::mx_max_splits(groups, T); }
+int r_rows_per_split(long long groups, int T, int longest, int dh) { return cca::mx_rows_per_split(groups, T, longest, dh); }
+}
+"""
+with tempfile.TemporaryDirectory() as tmp:
+    with open(os.path.join(tmp, "r.cpp"), "w") as f:
+        f.write(SOURCE)
+    subprocess.run(["g++", "-O1", "-std=c++17", "-shared", "-fPIC", "-I", os.path.join(ROOT, "paper_2510_04476_amd", "csrc"),
+                    os.path.join(tmp, "r.cpp"), "-o", os.path.join(tmp, "r.so")], check=True)
+    _lib = C.CDLL(os.path.join(tmp, "r.so"))
+
+
+def max_splits(groups, T):
+    return _lib.r_max_splits(C.c_longlong(groups), T)
+
+
+def rows_per_split(groups, T, longest, dh):
+    return _lib.r_rows_per_split(C.c_longlong(groups), T, longest, dh)

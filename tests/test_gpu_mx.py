@@ -1,0 +1,506 @@
+"""GPU parity of the 4-bit serving operators against mx_plain.py (64 bits), at the sizes and contents where they can go wrong.
+
+Bounds are worst cases counted in roundings.  u = 2^-24.  A score is a sum of d_h exact products in fp32: off by at most (d_h + 8)
+u sum|q k| scale, its exponential by as much and 2^-21 more; a probability enters the product with 16 bits (bf16 storage, in
+two parts; off by 2^-16) or 22 and more (fp32); n products are summed: n u.  A stored bf16 result is off by half a step, 2^-8."""
+import math
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+import mx_plain as X
+import paper_2510_04476_amd as P
+from oracle import cca_oracle as O
+from paper_2510_04476_amd import binding as B
+from synth_inputs import make_inputs
+from util import check_out, to_np
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+def say(*a):
+    print(*a, flush=True)
+    sys.stdout.flush()
+
+
+def config(B_=2, T=64, Hq=4, Hk=2, dh=64, dtype="bf16", **kw):
+    return P.CCAConfig(B=B_, T=T, d_model=Hq * dh, n_q_heads=Hq, n_kv_heads=Hk, head_dim=dh, dtype=B.CCA_F32 if dtype == "f32" else B.CCA_BF16, **kw)
+
+
+def i32(v):
+    return torch.tensor(np.asarray(v), dtype=torch.int32, device="cuda")
+
+
+def random_cache(cfg, seed, lens=None, tail_scale=255):
+    """A cache of stored random rows; what lies behind lens[b] has NaN scales.  Also its values, (B, Hk, T, dh) in 64 bits."""
+    rng = np.random.default_rng(seed)
+    shape = (cfg.B, cfg.n_kv_heads, cfg.T, cfg.head_dim)
+    parts, vals = [], []
+    for _ in range(2):
+        c, s = X.store(rng.standard_normal(shape) * np.exp(rng.standard_normal(shape[:3] + (1,))))
+        if lens is not None:
+            s[np.broadcast_to((np.arange(cfg.T) >= np.asarray(lens)[:, None])[:, None, :, None], s.shape)] = tail_scale
+        vals.append(X.values(c, s))
+        parts += [torch.from_numpy(c).cuda(), torch.from_numpy(np.ascontiguousarray(s.swapaxes(2, 3))).cuda()]
+    pos = torch.arange(cfg.T, dtype=torch.int32, device="cuda").expand(shape[:3]).contiguous()
+    weight = torch.from_numpy(rng.random(shape[:3], dtype=np.float32)).cuda()
+    return P.CCAMXCache(*parts, pos, weight), vals
+
+
+def rounded(a, dtype):
+    return torch.from_numpy(np.asarray(a, np.float32)).to(torch.float32 if dtype == "f32" else torch.bfloat16)
+
+
+def within(got, ref, bound, what):
+    got = to_np(got) if torch.is_tensor(got) else got
+    assert np.array_equal(np.isnan(got), np.isnan(ref)) and np.array_equal(np.isinf(got), np.isinf(ref)), what
+    with np.errstate(invalid="ignore"):
+        over = np.where(np.isfinite(ref), np.abs(got - ref) - bound, 0)
+    worst = float(over.max()) if over.size else 0.0
+    assert worst <= 0, (what, worst, np.unravel_index(over.argmax(), over.shape), got.flat[over.argmax()], ref.flat[over.argmax()])
+
+
+def check_attention(cfg, vals, q, lens, o, lse, weight=None, weight_in=None, weight_before=None):
+    Bn, Hk, dh, R = cfg.B, cfg.n_kv_heads, cfg.head_dim, cfg.n_q_heads // cfg.n_kv_heads
+    scale = cfg.softmax_scale or 1 / math.sqrt(dh)
+    q, o, lse = to_np(q), to_np(o).reshape(Bn, Hk, R, dh), to_np(lse).reshape(Bn, Hk, R)
+    for b in range(Bn):
+        n = int(lens[b])
+        for g in range(Hk):
+            k, v, qq = vals[0][b, g, :n], vals[1][b, g, :n], q[b, g * R:(g + 1) * R]
+            ro, rl, rp = X.attend(qq, k, v, scale)
+            with np.errstate(invalid="ignore"):
+                ds = (dh + 8) * U * (np.abs(qq) @ np.abs(k).T * scale).max(-1, keepdims=True) if n else np.zeros((R, 1))
+                dp = 2 * ds + 2.0 ** -20 + n * U
+                bo = (dp + (2.0 ** -16 if cfg.dtype == B.CCA_BF16 else 2.0 ** -22) + n * U) * (rp @ np.abs(v)) + np.abs(ro) * (2.0 ** -8 if cfg.dtype == B.CCA_BF16 else U)
+                within(o[b, g], ro, bo + 1e-30, ("o", b, g, n))
+                within(lse[b, g], rl, (dp + 4 * U * np.abs(rl)[:, None])[:, 0], ("lse", b, g, n))
+                if weight is not None:
+                    want = rp.sum(0) + (0 if weight_in is None else to_np(weight_in[b, g, :n]))
+                    within(weight[b, g, :n], want, (dp * rp).sum(0) + 2 * R * U * np.abs(want) + 1e-30, ("weight", b, g, n))
+                    assert torch.equal(weight[b, g, n:], weight_before[b, g, n:]), "rows behind the last one changed"
+
+
+# (B, T, lens, Hq, Hk, dh, dtype): every head width, 1 ... 40 query heads to a KV head, empty sequences, one row, ends inside a block, a
+# wavefront's round and a split, several splits
+ATTENTION = [
+    (3, 64, [0, 1, 64], 4, 2, 64, "bf16"), (2, 96, [33, 95], 3, 3, 32, "bf16"), (2, 320, [257, 256], 16, 2, 128, "bf16"),
+    (1, 1120, [1111], 12, 1, 128, "bf16"), (2, 2048, [2048, 5], 6, 2, 256, "bf16"), (1, 736, [700], 40, 1, 64, "bf16"),
+    (2, 160, [129, 0], 4, 2, 96, "bf16"), (2, 160, [160, 31], 2, 1, 160, "bf16"), (1, 320, [290], 9, 1, 192, "bf16"), (1, 96, [65], 3, 1, 224, "bf16"),
+    (2, 64, [0, 63], 4, 2, 32, "f32"), (1, 1056, [1030], 20, 1, 64, "f32"), (2, 288, [288, 17], 4, 4, 128, "f32"), (1, 544, [513], 2, 1, 256, "f32"),
+    (1, 96, [90], 5, 1, 96, "f32"), (9, 4096, [4096, 0, 1, 777, 2049, 4000, 64, 63, 1025], 8, 2, 64, "bf16"),
+]
+
+
+@pytest.mark.parametrize("i", range(len(ATTENTION)))
+def test_attention(i):
+    Bn, T, lens, Hq, Hk, dh, dt = ATTENTION[i]
+    say("case attention", ATTENTION[i])
+    cfg = config(Bn, T, Hq, Hk, dh, dt)
+    cache, vals = random_cache(cfg, 100 + i, lens)
+    q = rounded(np.random.default_rng(i).standard_normal((Bn, Hq, dh)), dt).cuda()
+    before = torch.full_like(cache.weight, 7.0)
+    w = before.clone()
+    o, lse = P.cca_decode_attention_mx(cfg, cache, q, i32(lens), T, want_lse=True, weight_in=cache.weight, weight_out=w)
+    torch.cuda.synchronize()
+    check_attention(cfg, vals, q, lens, o, lse, w, cache.weight, before)
+    # without weights, with the least bound on the lengths, and with fresh weights: the same
+    o2, lse2 = P.cca_decode_attention_mx(cfg, cache, q, i32(lens), T, want_lse=True)
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+    o3, lse3 = P.cca_decode_attention_mx(cfg, cache, q, i32(lens), max(lens), want_lse=True, weight_out=w.copy_(before))
+    torch.cuda.synchronize()
+    check_attention(cfg, vals, q, lens, o3, lse3, w, None, before)
+
+
+def test_attention_contents():
+    """NaN and infinite queries, a NaN group among the rows (its sequence and head alone are NaN), scores far apart, lengths out of range
+    (clamped), weights in place."""
+    cfg = config(4, 320, 4, 2, 64)
+    lens = [300, 320, 70, 5]
+    cache, vals = random_cache(cfg, 3, lens)
+    cache.k_scales[1, 0, 1, 200] = 255
+    vals[0][1, 0, 200, 32:] = np.nan
+    cache.k_scales[2, 1, :, 40] += 7  # one row's scores dominate
+    vals[0][2, 1, 40] *= 128
+    q = rounded(np.random.default_rng(5).standard_normal((4, 4, 64)), "bf16").cuda()
+    q[3, 3, 9] = float("nan")
+    w = cache.weight.clone()
+    o, lse = P.cca_decode_attention_mx(cfg, cache, q, i32([300, 100000, 70, 5]), 320, want_lse=True, weight_in=w, weight_out=w)
+    torch.cuda.synchronize()
+    check_attention(cfg, vals, q, lens, o, lse, w, cache.weight, cache.weight)
+    assert torch.isnan(o.view(4, 2, 128)[1, 0]).all() and torch.isfinite(o.view(4, 2, 128)[1, 1]).all()
+    o, lse = P.cca_decode_attention_mx(cfg, cache, q, i32([-5, 0, -(2 ** 31), 4]), 4, want_lse=True)
+    assert (o[:3] == 0).all() and torch.isneginf(lse[:3]).all() and torch.isfinite(o[3, :128].float()).all()
+    cfg0 = config(4, 320, 4, 2, 64, softmax_scale=0.5)
+    o, lse = P.cca_decode_attention_mx(cfg0, cache, q, i32([300, 0, 70, 0]), 300, want_lse=True)
+    torch.cuda.synchronize()
+    check_attention(cfg0, vals, q, [300, 0, 70, 0], o, lse)
+
+
+def test_attention_beyond_32_bit_offsets():
+    """A cache whose second head begins 2^32 bytes in; the last row of it and one in the middle hold all the weight."""
+    T = 1 << 25
+    cfg = config(1, T, 2, 2, 256)
+    cache = P.CCAMXCache.allocate(cfg, "cuda", with_weights=False)
+    assert cache.k_codes.numel() > 2 ** 32 + 2 ** 31
+    cache.k_scales.fill_(127)
+    cache.v_scales.fill_(127)
+    q = torch.ones(1, 2, 256, dtype=torch.bfloat16, device="cuda")
+    for head, row, code in ((0, T // 3, 0x22), (1, T - 1, 0x33), (1, T // 2, 0x33)):
+        cache.k_codes[0, head, row] = 0x77  # 6: a score of 96
+        cache.v_codes[0, head, row] = code  # 1, 1.5
+    cache.v_codes[0, 1, T // 2] = 0x55      # 3
+    w = torch.zeros(1, 2, T, device="cuda")
+    o, lse = P.cca_decode_attention_mx(cfg, cache, q, i32([T]), T, want_lse=True, weight_out=w)
+    torch.cuda.synchronize()
+    # the other rows' share: T e^-96
+    assert (o[0, :256] == 1.0).all() and (o[0, 256:] == 2.25).all()
+    assert abs(float(lse[0, 0]) - 96) < 1e-4 and abs(float(lse[0, 1]) - 96 - math.log(2)) < 1e-4
+    assert float(w[0, 0, T // 3]) == 1 and float(w[0, 1, T - 1]) == 0.5 and float(w[0, 1, T // 2]) == 0.5
+    k, v = P.cca_cache_rows_mx(cfg, cache, 2, first=i32([T - 1]))
+    assert (k[0, 0, 1] == 6).all() and (v[0, 0, 1] == 1.5).all() and (k[0, 1] == 0).all()
+
+
+# (B, T, n, rows, counts, Hk, dh, dtype)
+APPEND = [
+    (3, 96, 1, [0, 95, 40], None, 2, 64, "bf16"), (2, 256, 200, [0, 56], None, 2, 128, "bf16"), (3, 64, 40, [30, 64, -3], [40, 40, 7], 3, 32, "bf16"),
+    (2, 160, 70, [1, 90], [70, 0], 1, 96, "f32"), (1, 1024, 1000, [13], None, 4, 256, "bf16"), (2, 64, 64, [0, 0], [100, -1], 2, 160, "f32"), (1, 32, 32, [0], None, 1, 224, "bf16"),
+]
+
+
+@pytest.mark.parametrize("i", range(len(APPEND)))
+def test_append_and_read_back(i):
+    Bn, T, n, rows, counts, Hk, dh, dt = APPEND[i]
+    say("case append", APPEND[i])
+    cfg = config(Bn, T, Hk, Hk, dh, dt)
+    cache, _ = random_cache(cfg, 200 + i)
+    rng = np.random.default_rng(i)
+    new = []
+    for _ in range(2):
+        x = rng.standard_normal((Bn, n, Hk, dh)) * np.exp2(rng.integers(-20, 20, (Bn, n, Hk, 1)).astype(float))
+        x = np.array(x, np.float32)
+        x[0, 0, 0, :4] = [0.0, -0.0, 1e-30, -1e-38]
+        x[0, 0, 0, 4:32] = 0
+        if n > 10:
+            x[0, 3, 0, 5], x[0, 4, 0, 31], x[0, 5, 0, 1] = np.nan, -np.inf, 3.3e38
+            x[0, 6, 0, :32] = np.linspace(-7, 7, 32)
+            x[0, 7, 0, :32] = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5, 6] * 4)
+        new.append(rounded(x, dt))
+    want = [(getattr(cache, f + "_codes").cpu().numpy(), getattr(cache, f + "_scales").cpu().numpy(), x) for f, x in zip("kv", new)]
+    pos, weight = cache.pos.clone(), cache.weight.clone()
+    first = i32(rng.integers(0, 1000, Bn))
+    P.cca_cache_append_mx(cfg, cache, new[0].cuda(), new[1].cuda(), i32(rows), pos=first, counts=None if counts is None else i32(counts))
+    live = []
+    for b in range(Bn):
+        r = min(max(rows[b], 0), T)
+        live.append((r, max(0, min(n if counts is None else min(max(counts[b], 0), n), T - r))))
+    for codes, scales, x in want:
+        c, s = X.store(to_np(x))
+        for b, (r, m) in enumerate(live):
+            codes[b, :, r:r + m] = c[b, :m].swapaxes(0, 1)
+            scales[b, :, :, r:r + m] = s[b, :m].transpose(1, 2, 0)
+    for b, (r, m) in enumerate(live):
+        pos[b, :, r:r + m] = torch.arange(m, dtype=torch.int32, device="cuda") + first[b]
+        weight[b, :, r:r + m] = 0
+    torch.cuda.synchronize()
+    for f, (codes, scales, _) in zip("kv", want):
+        assert np.array_equal(getattr(cache, f + "_codes").cpu().numpy(), codes), f
+        assert np.array_equal(getattr(cache, f + "_scales").cpu().numpy(), scales), f
+    assert torch.equal(cache.pos, pos) and torch.equal(cache.weight, weight)
+    got = P.cca_cache_rows_mx(cfg, cache, n, first=i32(rows), count=None if counts is None else i32(counts))
+    for x, (codes, scales, _) in zip(got, want):
+        ref = np.zeros((Bn, n, Hk, dh))
+        for b, (r, m) in enumerate(live):
+            ref[b, :m] = X.values(codes[b, :, r:r + m], scales[b, :, :, r:r + m].swapaxes(1, 2)).swapaxes(0, 1)
+        assert np.array_equal(to_np(x), ref, equal_nan=True)
+
+
+def test_append_without_positions_and_every_scale_reads_back():
+    cfg = config(1, 256, 1, 1, 32, "f32")
+    cache = P.CCAMXCache.allocate(cfg, "cuda", with_weights=False)
+    cache.k_scales.copy_(torch.arange(256, dtype=torch.uint8, device="cuda").view(1, 1, 1, 256))
+    cache.k_codes.copy_(torch.arange(16, dtype=torch.uint8, device="cuda") * 17)
+    k, v = P.cca_cache_rows_mx(cfg, cache, 256)
+    ref = X.values(cache.k_codes.cpu().numpy()[0, 0], np.arange(256, dtype=np.uint8)[:, None])
+    with np.errstate(over="ignore"):
+        assert np.array_equal(to_np(k)[0, :, 0], ref.astype(np.float32).astype(np.float64), equal_nan=True)
+    x = torch.randn(1, 5, 1, 32, device="cuda")
+    P.cca_cache_append_mx(cfg, cache, x, x, i32([251]))
+    k, v = P.cca_cache_rows_mx(cfg, cache, 5, first=i32([251]))
+    assert torch.equal(k, v) and np.array_equal(to_np(k), X.values(*X.store(to_np(x))))
+
+
+# (B, T, lens, Hk, dh, budget, recent)
+EVICT = [
+    (1, 64, [64], 1, 32, 40, 8), (4, 96, [96, 0, 50, 51], 2, 64, 50, 0), (2, 320, [320, 300], 2, 128, 1, 1), (2, 320, [319, 77], 2, 96, 318, 318),
+    (1, 3008, [3001], 3, 64, 1500, 100), (3, 8192, [8192, 4097, 8000], 2, 256, 4096, 17), (1, 40000, [39999], 2, 32, 555, 55), (1, 4096, [4096], 1, 64, 4096, 0), (1, 128, [100], 1, 32, 128, 1),
+]
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("i", range(len(EVICT)))
+def test_evict(i, in_place):
+    Bn, T, lens, Hk, dh, budget, recent = EVICT[i]
+    say("case evict", EVICT[i], in_place)
+    cfg = config(Bn, T, Hk, Hk, dh)
+    cache, _ = random_cache(cfg, 300 + i)
+    rng = np.random.default_rng(i)
+    w = rng.standard_normal((Bn, Hk, T)).astype(np.float32)
+    w[..., ::3] = np.round(w[..., ::3])                  # many equal ones, -0 and 0 among them
+    w[0, 0, 5:9] = [np.nan, np.inf, -np.inf, -0.0]
+    p = np.stack([[rng.permutation(T) for _ in range(Hk)] for _ in range(Bn)]).astype(np.int32)  # as earlier evictions leave them
+    cache.weight.copy_(torch.from_numpy(w))
+    cache.pos.copy_(torch.from_numpy(p))
+    old = {f: getattr(cache, f).cpu().numpy().copy() for f in ("k_codes", "k_scales", "v_codes", "v_scales")}
+    n, out = i32(lens), {}
+    if not in_place:
+        out = dict(weight_out=torch.full_like(cache.weight, 9.0), pos_out=torch.full_like(cache.pos, 9), lens_out=torch.full_like(n, 9))
+    P.cca_cache_evict_mx(cfg, cache, n, T, budget, recent, **out)
+    torch.cuda.synchronize()
+    wo, po, no = (out["weight_out"], out["pos_out"], out["lens_out"]) if out else (cache.weight, cache.pos, n)
+    assert no.tolist() == [min(x, budget) for x in lens]
+    if out:
+        assert n.tolist() == lens and np.array_equal(cache.weight.cpu().numpy(), w, equal_nan=True) and np.array_equal(cache.pos.cpu().numpy(), p)
+    for b in range(Bn):
+        for g in range(Hk):
+            src = X.evict(w[b, g], p[b, g], lens[b], budget, recent)
+            m = len(src)
+            assert np.array_equal(wo[b, g, :m].cpu().numpy(), w[b, g, src], equal_nan=True) and np.array_equal(po[b, g, :m].cpu().numpy(), p[b, g, src]), (b, g)
+            for f in ("k", "v"):
+                assert np.array_equal(getattr(cache, f + "_codes")[b, g, :m].cpu().numpy(), old[f + "_codes"][b, g, src]), (f, b, g)
+                assert np.array_equal(getattr(cache, f + "_scales")[b, g, :, :m].cpu().numpy(), old[f + "_scales"][b, g][:, src]), (f, b, g)
+            if out:
+                assert (wo[b, g, m:] == 9).all() and (po[b, g, m:] == 9).all()
+
+
+def test_evict_ranks_by_position_then_weight_then_row():
+    cfg = config(2, 64, 1, 1, 32)
+    cache, _ = random_cache(cfg, 1)
+    cache.weight.fill_(0.5)                       # all equal: the first rows stay, but for the recent ones
+    cache.pos[1].copy_(cache.pos[1].flip(-1))        # the newest token in row 0
+    cache.pos.add_(2 ** 31 - 65)                   # up to the largest position there is
+    n = i32([64, 1000])
+    P.cca_cache_evict_mx(cfg, cache, n, 64, 10, 4)
+    top = 2 ** 31 - 2
+    assert n.tolist() == [10, 10]
+    assert (top - cache.pos[0, 0, :10]).tolist() == [63, 62, 61, 60, 59, 58, 3, 2, 1, 0]
+    assert (top - cache.pos[1, 0, :10]).tolist() == list(range(10))
+
+
+PROJECT = [(1, 32, 1), (1, 2048, 1536), (16, 96, 33), (17, 1056, 47), (32, 4096, 512), (33, 64, 200), (65, 288, 130), (3, 8192, 16), (128, 160, 300), (5, 32, 4100)]
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("i", range(len(PROJECT)))
+def test_project(i, dt):
+    M, K, N = PROJECT[i]
+    say("case project", PROJECT[i], dt)
+    rng = np.random.default_rng(i)
+    w = rounded(rng.standard_normal((K, N)) / math.sqrt(K), dt)
+    x = rounded(rng.standard_normal((M, K)), dt)
+    q = P.cca_mx_quantize(w.cuda())
+    codes, scales = X.store(to_np(w).T.copy())
+    assert np.array_equal(q.codes.cpu().numpy(), codes) and np.array_equal(q.scales.cpu().numpy(), scales)
+    ref_w = X.values(codes, scales).T
+    y = P.cca_project_mx(x.cuda(), q)
+    ref = to_np(x) @ ref_w
+    # three parts of x in fp32: 24 bits; 3 K sums
+    bound = (3 * K + 8) * U * (np.abs(to_np(x)) @ np.abs(ref_w)) + np.abs(ref) * (2.0 ** -8 if dt == "bf16" else U)
+    within(y, ref, bound, "y")
+    out = torch.full((M + 2, N + 0), 3.0, dtype=x.dtype, device="cuda")
+    if (2 * N * out.element_size()) % 16 == 0 or M == 1:
+        P.cca_project_mx(x.cuda(), q, out=out[:M])
+        assert torch.equal(out[:M], y) and (out[M:] == 3).all()
+
+
+def test_project_contents():
+    """NaN and infinite inputs stay in their row, a NaN group in its column; leading dimensions are kept."""
+    rng = np.random.default_rng(1)
+    q = P.cca_mx_quantize(rounded(rng.standard_normal((96, 40)), "bf16").cuda())
+    q.scales[7, 1] = 255
+    x = rounded(rng.standard_normal((2, 3, 96)), "bf16").cuda()
+    x[0, 1, 95], x[1, 2, 0] = float("nan"), float("inf")
+    y = P.cca_project_mx(x, q)
+    assert y.shape == (2, 3, 40)
+    bad = torch.zeros(2, 3, 40, dtype=torch.bool, device="cuda")
+    bad[0, 1] = True
+    bad[..., 7] = True
+    assert torch.isnan(y)[bad].all() and torch.isfinite(y[0, 0, :7]).all() and torch.isfinite(y[1, 1, 8:]).all()
+    assert not torch.isfinite(y[1, 2]).any() or (~torch.isfinite(y[1, 2])).sum() >= 35
+
+
+# ---- the operators together ------------------------------------------------------------------------------------------
+
+STEP = [
+    dict(B=2, T=96, E=256, Hq=4, Hk=2, dh=32, k_seq=2, k_ch=2, dtype="f32", paper_flags=True),
+    dict(B=3, T=128, E=1024, Hq=8, Hk=2, dh=128, k_seq=2, k_ch=2, dtype="bf16", paper_flags=True),
+    dict(B=1, T=64, E=512, Hq=2, Hk=1, dh=256, k_seq=3, k_ch=1, dtype="bf16", paper_flags=True),
+    dict(B=2, T=64, E=512, Hq=4, Hk=2, dh=64, k_seq=1, k_ch=1, dtype="bf16", paper_flags=False),
+]
+
+
+def step_setup(w, seed):
+    """The layer's inputs and weights with both projections in 4 bits, on the device and as the oracle takes them."""
+    inp = make_inputs(w, seed=seed, conv_visible=True)
+    cfg = P.config_from_workload(w)
+    x, wt = P.weights_to_device(cfg, inp)
+    down, up = P.cca_mx_quantize(wt.w_down), P.cca_mx_quantize(wt.w_out)
+    wq = {}
+    for name, q in (("w_down", down), ("w_out", up)):
+        wq[name] = X.values(q.codes.cpu().numpy(), q.scales.cpu().numpy()).T
+        assert np.array_equal(wq[name], X.values(*X.store(inp[name].T.astype(np.float64).copy())).T)
+    flags = {} if w["paper_flags"] else dict(use_conv_seq=False, use_conv_ch=False, use_qk_mean=False, use_v_shift=False, use_qk_norm=False,
+                                             use_key_temp=False, use_rope=False)
+    ref = O.cca_forward(inp["x"], wq["w_down"], inp["w_conv_seq"], inp["w_conv_ch"], inp["temp"], wq["w_out"], n_q_heads=w["Hq"],
+                        n_kv_heads=w["Hk"], head_dim=w["dh"], **flags)
+    return cfg, x, wt, down, up, wq, ref
+
+
+@pytest.mark.parametrize("i", range(len(STEP)))
+def test_steps_with_eviction_between(i):
+    """A sequence token by token from a prefill, evicted twice on the way.  Each step's new row is the oracle's key and value as the
+    format keeps them; its output is the oracle's query over the rows that the cache then holds; its weights are those probabilities."""
+    w = STEP[i]
+    say("case steps", w)
+    cfg, x, wt, down, up, wq, ref = step_setup(w, 60 + i)
+    Bn, T, Hk, R, dh = w["B"], w["T"], w["Hk"], w["Hq"] // w["Hk"], w["dh"]
+    start = 20
+    pre = P.config_from_workload(dict(w, T=start))
+    # the prefill runs on the weights that the 4-bit ones stand for (bf16 numbers)
+    dev = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to("cuda", cfg.torch_dtype)
+    wd = P.CCAWeights(w_down=dev(wq["w_down"]), w_out=dev(wq["w_out"]), w_conv_seq=wt.w_conv_seq, w_conv_ch=wt.w_conv_ch,
+                      temp=wt.temp)
+    saved = P.CCASaved.allocate(pre, "cuda")
+    P.cca_forward(pre, wd, x[:, :start].contiguous(), saved=saved)
+    state = P.CCADecodeStateMX.allocate(cfg, "cuda")
+    state.load_prefill(cfg, saved, start)
+    lens, pos = i32([start] * Bn), i32([start] * Bn)
+    scale = 1 / math.sqrt(dh)
+    tol = 1e-2 if w["dtype"] == "bf16" else 1e-5
+    for t in range(start, 52):
+        if t in (30, 45):
+            P.cca_cache_evict_mx(cfg, state.cache, lens, T, 18, 6, workspace=state.workspace)
+            assert lens.tolist() == [18] * Bn
+            assert state.cache.pos[:, :, :18].max() == t - 1
+        before = state.cache.weight.clone()
+        n = int(lens[0])
+        out = P.cca_decode_step_mx(cfg, wt, down, up, x[:, t].contiguous(), state, pos, lens, T - 1)
+        k, v = (to_np(a) for a in P.cca_cache_rows_mx(cfg, state.cache, n + 1))
+        weight, rowpos = to_np(state.cache.weight), state.cache.pos.cpu().numpy()
+        for new, name in ((k[:, n], "k"), (v[:, n], "v")):
+            amax = np.abs(ref[name][:, t].reshape(Bn, Hk, dh // 32, 32)).max(-1, keepdims=True)
+            # a fifth of the group's largest for the format, and the layer's own rounding in front of it
+            assert (np.abs(new - ref[name][:, t]).reshape(Bn, Hk, dh // 32, 32) <= amax * (0.2 + 3 * tol)).all(), name
+        assert (rowpos[:, :, n] == t).all()
+        got, o = to_np(out), np.zeros((Bn, Hk * R * dh))
+        for b in range(Bn):
+            for g in range(Hk):
+                oo, _, p = X.attend(ref["q"][b, t, g * R:(g + 1) * R], k[b, :, g], v[b, :, g], scale)
+                o[b, g * R * dh:(g + 1) * R * dh] = oo.ravel()
+                grow = weight[b, g, :n + 1] - np.append(to_np(before[b, g, :n]), 0.0)
+                assert np.abs(grow - p.sum(0)).max() <= 8 * tol * max(1.0, p.sum(0).max()), (t, b, g)
+        assert (weight[:, :, n + 1:] == to_np(before)[:, :, n + 1:]).all()
+        check_out(got, o @ wq["w_out"], w["dtype"], f"step at {t}")
+        lens += 1
+        pos += 1
+
+
+def test_step_of_sequences_at_different_lengths_equals_single_ones():
+    w = STEP[1]
+    cfg, x, wt, down, up, _, _ = step_setup(w, 77)
+    one = P.config_from_workload(dict(w, B=1))
+    lens, pos = [0, 127, 63], [0, 500, 64]
+    states, outs = [], []
+    batch = P.CCADecodeStateMX.allocate(cfg, "cuda")
+    filled, _ = random_cache(cfg, 9)
+    for f in ("k_codes", "k_scales", "v_codes", "v_scales", "pos", "weight"):
+        getattr(batch.cache, f).copy_(getattr(filled, f))
+    batch.lat_ring.normal_()
+    for b in range(3):
+        s = P.CCADecodeStateMX.allocate(one, "cuda")
+        for f in ("k_codes", "k_scales", "v_codes", "v_scales", "pos", "weight"):
+            getattr(s.cache, f).copy_(getattr(filled, f)[b:b + 1])
+        s.lat_ring.copy_(batch.lat_ring[b:b + 1])
+        outs.append(P.cca_decode_step_mx(one, wt, down, up, x[b:b + 1, 0].contiguous(), s, i32([pos[b]]), i32([lens[b]]), 127))
+        states.append(s)
+    out = P.cca_decode_step_mx(cfg, wt, down, up, x[:, 0].contiguous(), batch, i32(pos), i32(lens), 127)
+    torch.cuda.synchronize()
+    for b, s in enumerate(states):
+        for f in ("k_codes", "k_scales", "v_codes", "v_scales", "pos"):
+            assert torch.equal(getattr(batch.cache, f)[b:b + 1], getattr(s.cache, f)), (b, f)
+        assert torch.equal(batch.lat_ring[b:b + 1], s.lat_ring)
+        # (the splits of a row range depend on the batch: equal up to the order of sums)
+        assert (out[b].float() - outs[b][0].float()).abs().max() <= 2.0 ** -7 * outs[b].float().abs().max()
+        assert (batch.cache.weight[b] - s.cache.weight[0]).abs().max() <= 1e-5
+    # a length beyond the bound is clamped: the row lands inside the cache
+    P.cca_decode_step_mx(cfg, wt, down, up, x[:, 0].contiguous(), batch, i32([2 ** 31 - 1, -7, 3]), i32([10 ** 9, -4, 5]), 127)
+    torch.cuda.synchronize()
+    assert batch.cache.pos[0, 0, 127] == 2 ** 31 - 1 and batch.cache.pos[1, 0, 0] == -7 and batch.cache.pos[2, 1, 5] == 3
+
+
+def test_calls_on_another_stream_and_in_graphs():
+    """Captured attention, eviction and step, replayed with eager calls between, and two graphs with workspaces of their own replayed in
+    turn: every replay gives the eager result bit for bit."""
+    w = STEP[1]
+    cfg, x, wt, down, up, _, _ = step_setup(w, 78)
+    side = torch.cuda.Stream()
+
+    def fresh():
+        s = P.CCADecodeStateMX.allocate(cfg, "cuda")
+        filled, _ = random_cache(cfg, 10)
+        for f in ("k_codes", "k_scales", "v_codes", "v_scales", "pos", "weight"):
+            getattr(s.cache, f).copy_(getattr(filled, f))
+        g = torch.Generator(device="cuda").manual_seed(3)
+        s.lat_ring.copy_(torch.randn(s.lat_ring.shape, generator=g, device="cuda"))
+        return s
+
+    pos, x_new = i32([100, 50, 90]), x[:, 0].contiguous()
+
+    def program(s, lens, out):
+        """One step, then an eviction; lens advances on the device."""
+        P.cca_decode_step_mx(cfg, wt, down, up, x_new, s, pos, lens, cfg.T - 1, out=out)
+        lens += 1
+        P.cca_cache_evict_mx(cfg, s.cache, lens, cfg.T, 40, 5, workspace=s.workspace)
+
+    start = [60, 39, 100]
+    eager, n_e, out_e = fresh(), i32(start), torch.empty_like(x_new)
+    states, lens, outs, graphs = [fresh(), fresh()], [i32(start), i32(start)], [torch.empty_like(x_new) for _ in range(2)], []
+    with torch.cuda.stream(side):  # warm-up of the capture stream, on a state of its own
+        program(fresh(), i32(start), torch.empty_like(x_new))
+    torch.cuda.synchronize()
+    for s, n, o in zip(states, lens, outs):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            program(s, n, o)
+        graphs.append(g)
+    torch.cuda.synchronize()
+    for rep in range(4):
+        program(eager, n_e, out_e)
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for s, n, o in zip(states, lens, outs):
+            assert torch.equal(o, out_e) and torch.equal(n, n_e), rep
+            for f in ("k_codes", "k_scales", "v_codes", "v_scales", "pos", "weight"):
+                assert torch.equal(getattr(s.cache, f)[:, :, :40], getattr(eager.cache, f)[:, :, :40]) if "scales" not in f else \
+                    torch.equal(getattr(s.cache, f)[..., :40], getattr(eager.cache, f)[..., :40]), (rep, f)
+    with torch.cuda.stream(side):
+        o2 = P.cca_project_mx(x_new, down)
+    torch.cuda.synchronize()
+    assert torch.equal(o2, P.cca_project_mx(x_new, down))
+
+
+def test_results_repeat_bit_for_bit():
+    cfg = config(5, 2048, 8, 2, 128)
+    lens = [2048, 0, 1500, 3, 700]
+    cache, _ = random_cache(cfg, 4, lens)
+    q = rounded(np.random.default_rng(2).standard_normal((5, 8, 128)), "bf16").cuda()
+    runs = []
+    for _ in range(3):
+        w = torch.zeros_like(cache.weight)
+        runs.append((*P.cca_decode_attention_mx(cfg, cache, q, i32(lens), 2048, want_lse=True, weight_out=w), w))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for r in runs[1:] for a, b in zip(runs[0], r))
