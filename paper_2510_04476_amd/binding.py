@@ -152,6 +152,22 @@ class CCAConfig:
                           self.n_kv_heads, self.head_dim, self.k_seq, self.k_ch, self.dtype, self.flags,
                           self.rope_base, self.softmax_scale, self.norm_eps)
 
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        self.__dict__.pop("_kept", None)
+
+    def ref(self):
+        """The C form by reference, made again after a field has changed."""
+        kept = self.__dict__.get("_kept")
+        if kept is None:
+            kept = self.__dict__["_kept"] = C.byref(self.c())
+        return kept
+
+    def ring_rows(self) -> int:
+        """Depth P of a decode state's latent ring (cca_decode_workspace_size reports the same)."""
+        taps = (self.k_seq if self.flags & CCA_CONV_SEQ else 1) + (self.k_ch if self.flags & CCA_CONV_CH else 1) - 1
+        return max(taps - 1, 1) + 1
+
     @property
     def torch_dtype(self):
         return torch.bfloat16 if self.dtype == CCA_BF16 else torch.float32
@@ -493,31 +509,35 @@ def cca_decode_step_static(cfg: CCAConfig, w: CCAWeights, x_new, state: CCADecod
 
 
 # ---- serving with 4 bits a number (format and layouts: cca.h) --------------
-def _mx_arg(name, t, shape, dtype, device):
-    """Address of `t` after the checks that the library cannot make."""
-    if t.device != device:
-        raise ValueError(f"{name}: on {t.device}, expected {device}")
-    if t.dtype != dtype or t.shape != shape:
-        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, expected {dtype} {tuple(shape)}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name}: libcca takes contiguous tensors")
+# A call of these takes a few microseconds on the GPU, so what Python spends on one counts: plain comparisons, the config's C form kept
+# until a field changes, the current stream's handle without a Stream object around it.
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _mx_ptr(name, t, shape, dtype, index):
+    """Address of `t` after the checks that the library cannot make (index: the device's, -1 for the CPU)."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}; expected a "
+                         f"contiguous {dtype} {tuple(shape)} on {'the CPU' if index < 0 else f'GPU {index}'}")
     return t.data_ptr()
 
 
-def _mx_rows_arg(name, t, cfg, device):
-    return None if t is None else _mx_arg(name, t, (cfg.B,), torch.int32, device)
+def _mx_opt(name, t, shape, dtype, index):
+    return None if t is None else _mx_ptr(name, t, shape, dtype, index)
 
 
-def _mx_call(where, device, *args):
+def _mx_call(where, index, *args):
     """A call on the tensors' device and on that device's current stream."""
-    if device.type != "cuda":
-        raise ValueError(f"{where}: tensors on {device}, expected a GPU")
-    fn = getattr(load_library(), where)
-    if device.index == torch.cuda.current_device():
-        _check(fn(*args, torch.cuda.current_stream().cuda_stream), where)
+    if index < 0:
+        raise ValueError(f"{where}: tensors on the CPU, expected a GPU")
+    fn = getattr(_lib or load_library(), where)
+    if index == torch._C._cuda_getDevice():
+        status = fn(*args, _raw_stream(index))
     else:
-        with torch.cuda.device(device):
-            _check(fn(*args, torch.cuda.current_stream().cuda_stream), where)
+        with torch.cuda.device(index):
+            status = fn(*args, _raw_stream(index))
+    if status:
+        raise CCAError(status, where)
 
 
 @dataclass(frozen=True)
@@ -527,18 +547,12 @@ class CCAMXWeight:
     scales: torch.Tensor
 
     def __post_init__(self):
-        n, k = self.codes.shape[0], 2 * self.codes.shape[1]
-        _mx_arg("codes", self.codes, (n, k // 2), torch.uint8, self.codes.device)
-        _mx_arg("scales", self.scales, (n, k // 32), torch.uint8, self.codes.device)
-        object.__setattr__(self, "_c", cca_mx_weight(self.codes.data_ptr(), self.scales.data_ptr()))
-
-    @property
-    def K(self):
-        return 2 * self.codes.shape[1]
-
-    @property
-    def N(self):
-        return self.codes.shape[0]
+        if self.codes.dim() != 2:
+            raise ValueError(f"codes: {tuple(self.codes.shape)}, expected (N, K/2)")
+        n, k, index = self.codes.shape[0], 2 * self.codes.shape[1], self.codes.get_device()
+        c = cca_mx_weight(_mx_ptr("codes", self.codes, (n, k // 2), torch.uint8, index), _mx_ptr("scales", self.scales, (n, k // 32), torch.uint8, index))
+        for name, v in (("K", k), ("N", n), ("_index", index), ("_c", c), ("_ref", C.byref(c))):
+            object.__setattr__(self, name, v)
 
 
 @dataclass(frozen=True)
@@ -556,14 +570,14 @@ class CCAMXCache:
         if self.k_codes.dim() != 4:
             raise ValueError(f"k_codes: {tuple(self.k_codes.shape)}, expected (B, H_k, T, d_h/2)")
         B, Hk, T, half = self.k_codes.shape
-        dev, ptrs = self.k_codes.device, {}
+        index, ptrs = self.k_codes.get_device(), {}
         for name, shape, dt in (("k_codes", (B, Hk, T, half), torch.uint8), ("v_codes", (B, Hk, T, half), torch.uint8),
                                 ("k_scales", (B, Hk, half // 16, T), torch.uint8), ("v_scales", (B, Hk, half // 16, T), torch.uint8),
                                 ("pos", (B, Hk, T), torch.int32), ("weight", (B, Hk, T), torch.float32)):
-            t = getattr(self, name)
-            ptrs[name] = None if t is None else _mx_arg(name, t, shape, dt, dev)
-        object.__setattr__(self, "_c", cca_mx_cache(**ptrs))
-        object.__setattr__(self, "_layout", (B, Hk, T, 2 * half))
+            ptrs[name] = _mx_opt(name, getattr(self, name), shape, dt, index)
+        c = cca_mx_cache(**ptrs)
+        for name, v in (("_index", index), ("_device", self.k_codes.device), ("_layout", (B, Hk, T, 2 * half)), ("_c", c), ("_ref", C.byref(c))):
+            object.__setattr__(self, name, v)
 
     @staticmethod
     def allocate(cfg: CCAConfig, device, with_weights: bool = True) -> "CCAMXCache":
@@ -576,7 +590,7 @@ class CCAMXCache:
     def _for(self, cfg: CCAConfig):
         if self._layout != (cfg.B, cfg.n_kv_heads, cfg.T, cfg.head_dim):
             raise ValueError(f"cache of (B, H_k, T, d_h) = {self._layout}, config of {(cfg.B, cfg.n_kv_heads, cfg.T, cfg.head_dim)}")
-        return C.byref(self._c)
+        return self._ref
 
 
 def cca_mx_workspace_size(cfg: CCAConfig) -> int:
@@ -596,43 +610,42 @@ def cca_mx_quantize(w: torch.Tensor) -> CCAMXWeight:
         raise ValueError(f"cca_mx_quantize: {w.dtype} {tuple(w.shape)}, expected a bf16 or fp32 matrix")
     K, N = w.shape
     q = CCAMXWeight(torch.empty(N, K // 2, dtype=torch.uint8, device=w.device), torch.empty(N, K // 32, dtype=torch.uint8, device=w.device))
-    _mx_call("cca_mx_quantize", w.device, _ptr(w), K, N, CCA_BF16 if w.dtype == torch.bfloat16 else CCA_F32, q.codes.data_ptr(),
+    _mx_call("cca_mx_quantize", w.get_device(), _ptr(w), K, N, CCA_BF16 if w.dtype == torch.bfloat16 else CCA_F32, q.codes.data_ptr(),
              q.scales.data_ptr())
     return q
 
 
 def cca_project_mx(x: torch.Tensor, w: CCAMXWeight, out: torch.Tensor | None = None) -> torch.Tensor:
     """x (..., K) W -> (..., N), in x's type (bf16 or fp32)."""
-    K, N, dev = w.K, w.N, w.codes.device
-    if x.dtype not in (torch.bfloat16, torch.float32) or x.dim() < 1 or x.shape[-1] != K:
-        raise ValueError(f"cca_project_mx: x {x.dtype} {tuple(x.shape)}, weight of K = {K}")
-    if out is None:
-        out = torch.empty(*x.shape[:-1], N, dtype=x.dtype, device=dev)
-    _mx_call("cca_project_mx", dev, _mx_arg("x", x, x.shape, x.dtype, dev), C.byref(w._c),
-             _mx_arg("out", out, (*x.shape[:-1], N), x.dtype, dev), x.numel() // K, K, N, CCA_BF16 if x.dtype == torch.bfloat16 else CCA_F32)
+    dt, shape, index = x.dtype, x.shape, w._index
+    if (dt is not torch.bfloat16 and dt is not torch.float32) or not shape or shape[-1] != w.K:
+        raise ValueError(f"cca_project_mx: x {dt} {tuple(shape)}, weight of K = {w.K}")
+    y_shape = (*shape[:-1], w.N)
+    out = x.new_empty(y_shape) if out is None else out
+    _mx_call("cca_project_mx", index, _mx_ptr("x", x, shape, dt, index), w._ref, _mx_ptr("out", out, y_shape, dt, index), x.numel() // w.K,
+             w.K, w.N, CCA_BF16 if dt is torch.bfloat16 else CCA_F32)
     return out
 
 
 def cca_cache_append_mx(cfg: CCAConfig, cache: CCAMXCache, k, v, rows, pos=None, counts=None) -> None:
     """Stores k, v (B, n, H_k, d_h) as rows rows[b] ... of every sequence, the first counts[b] of them (None: all), of tokens at
     positions pos[b] ... (None: the rows' numbers)."""
-    dev, dt = cache.k_codes.device, cfg.torch_dtype
+    index, dt, per_seq = cache._index, cfg.torch_dtype, (cfg.B,)
     n = k.shape[1] if k.dim() == 4 else 0
     shape = (cfg.B, n, cfg.n_kv_heads, cfg.head_dim)
-    cc = cfg.c()
-    _mx_call("cca_cache_append_mx", dev, C.byref(cc), cache._for(cfg), _mx_arg("k", k, shape, dt, dev), _mx_arg("v", v, shape, dt, dev), n,
-             _mx_rows_arg("rows", rows, cfg, dev), _mx_rows_arg("counts", counts, cfg, dev), _mx_rows_arg("pos", pos, cfg, dev))
+    _mx_call("cca_cache_append_mx", index, cfg.ref(), cache._for(cfg), _mx_ptr("k", k, shape, dt, index), _mx_ptr("v", v, shape, dt, index), n,
+             _mx_ptr("rows", rows, per_seq, torch.int32, index), _mx_opt("counts", counts, per_seq, torch.int32, index),
+             _mx_opt("pos", pos, per_seq, torch.int32, index))
 
 
 def cca_cache_rows_mx(cfg: CCAConfig, cache: CCAMXCache, n: int, first=None, count=None, k=None, v=None):
     """(k, v), (B, n, H_k, d_h): rows first[b] ... (None: 0 ...) of every sequence, zero from the count[b]-th on (None: none)."""
-    dev, dt = cache.k_codes.device, cfg.torch_dtype
+    index, dt, per_seq = cache._index, cfg.torch_dtype, (cfg.B,)
     shape = (cfg.B, n, cfg.n_kv_heads, cfg.head_dim)
-    k = torch.empty(shape, dtype=dt, device=dev) if k is None else k
-    v = torch.empty(shape, dtype=dt, device=dev) if v is None else v
-    cc = cfg.c()
-    _mx_call("cca_cache_rows_mx", dev, C.byref(cc), cache._for(cfg), _mx_arg("k", k, shape, dt, dev), _mx_arg("v", v, shape, dt, dev), n,
-             _mx_rows_arg("first", first, cfg, dev), _mx_rows_arg("count", count, cfg, dev))
+    k = torch.empty(shape, dtype=dt, device=cache._device) if k is None else k
+    v = torch.empty(shape, dtype=dt, device=cache._device) if v is None else v
+    _mx_call("cca_cache_rows_mx", index, cfg.ref(), cache._for(cfg), _mx_ptr("k", k, shape, dt, index), _mx_ptr("v", v, shape, dt, index), n,
+             _mx_opt("first", first, per_seq, torch.int32, index), _mx_opt("count", count, per_seq, torch.int32, index))
     return k, v
 
 
@@ -640,22 +653,19 @@ def cca_decode_attention_mx(cfg: CCAConfig, cache: CCAMXCache, q, lens, max_len:
                             weight_out=None, workspace=None):
     """o (B, H_q*d_h): attention of one query per sequence, q (B, H_q, d_h), over the first lens[b] <= max_len rows (int32 device
     tensor).  With weight_out (B, H_k, T) each of those rows' weight_in (None: 0) plus the attention it got goes there."""
-    dev, dt = cache.k_codes.device, cfg.torch_dtype
-    B, Hq = cfg.B, cfg.n_q_heads
+    index, dt, B, Hq, dh = cache._index, cfg.torch_dtype, cfg.B, cfg.n_q_heads, cfg.head_dim
     if o is None:
-        o = torch.empty(B, cfg.e_q, dtype=dt, device=dev)
+        o = torch.empty((B, Hq * dh), dtype=dt, device=cache._device)
     if lse is None and want_lse:
-        lse = torch.empty(B, Hq, dtype=torch.float32, device=dev)
+        lse = torch.empty((B, Hq), dtype=torch.float32, device=cache._device)
     if workspace is None:
-        workspace = new_mx_workspace(cfg, dev)
+        workspace = new_mx_workspace(cfg, cache._device)
     w = (B, cfg.n_kv_heads, cfg.T)
-    cc = cfg.c()
-    _mx_call("cca_decode_attention_mx", dev, C.byref(cc), cache._for(cfg), _mx_arg("q", q, (B, Hq, cfg.head_dim), dt, dev),
-             _mx_rows_arg("lens", lens, cfg, dev), max_len, _mx_arg("o", o, (B, cfg.e_q), dt, dev),
-             None if lse is None else _mx_arg("lse", lse, (B, Hq), torch.float32, dev),
-             None if weight_in is None else _mx_arg("weight_in", weight_in, w, torch.float32, dev),
-             None if weight_out is None else _mx_arg("weight_out", weight_out, w, torch.float32, dev),
-             _mx_arg("workspace", workspace, workspace.shape, torch.uint8, dev), workspace.numel())
+    _mx_call("cca_decode_attention_mx", index, cfg.ref(), cache._for(cfg), _mx_ptr("q", q, (B, Hq, dh), dt, index),
+             _mx_ptr("lens", lens, (B,), torch.int32, index), max_len, _mx_ptr("o", o, (B, Hq * dh), dt, index),
+             _mx_opt("lse", lse, (B, Hq), torch.float32, index), _mx_opt("weight_in", weight_in, w, torch.float32, index),
+             _mx_opt("weight_out", weight_out, w, torch.float32, index),
+             _mx_ptr("workspace", workspace, workspace.shape, torch.uint8, index), workspace.numel())
     return (o, lse) if want_lse else o
 
 
@@ -663,15 +673,14 @@ def cca_cache_evict_mx(cfg: CCAConfig, cache: CCAMXCache, lens, max_len: int, bu
                        lens_out=None, workspace=None) -> None:
     """Keeps at most `budget` rows of every head: the tokens of the last `recent` positions, then the rows of greatest weight.  Updates
     cache.pos, cache.weight and lens in place, or leaves them and writes pos_out, weight_out, lens_out."""
-    dev = cache.k_codes.device
+    index = cache._index
     if workspace is None:
-        workspace = new_mx_workspace(cfg, dev)
+        workspace = new_mx_workspace(cfg, cache._device)
     w = (cfg.B, cfg.n_kv_heads, cfg.T)
-    cc = cfg.c()
-    _mx_call("cca_cache_evict_mx", dev, C.byref(cc), cache._for(cfg), _mx_rows_arg("lens", lens, cfg, dev), max_len, budget, recent,
-             None if weight_out is None else _mx_arg("weight_out", weight_out, w, torch.float32, dev),
-             None if pos_out is None else _mx_arg("pos_out", pos_out, w, torch.int32, dev), _mx_rows_arg("lens_out", lens_out, cfg, dev),
-             _mx_arg("workspace", workspace, workspace.shape, torch.uint8, dev), workspace.numel())
+    _mx_call("cca_cache_evict_mx", index, cfg.ref(), cache._for(cfg), _mx_ptr("lens", lens, (cfg.B,), torch.int32, index), max_len, budget,
+             recent, _mx_opt("weight_out", weight_out, w, torch.float32, index), _mx_opt("pos_out", pos_out, w, torch.int32, index),
+             _mx_opt("lens_out", lens_out, (cfg.B,), torch.int32, index),
+             _mx_ptr("workspace", workspace, workspace.shape, torch.uint8, index), workspace.numel())
 
 
 @dataclass
@@ -700,21 +709,17 @@ def cca_decode_step_mx(cfg: CCAConfig, w: CCAWeights, w_down: CCAMXWeight, w_out
                        max_len: int, out=None):
     """out (B, E) for the new token of each sequence, at position pos[b] of its text; it becomes row lens[b] <= max_len of the cache (both
     int32 device tensors, not advanced).  Of `w` the convolution filters and the temperatures are read."""
-    dev, dt = state.cache.k_codes.device, cfg.torch_dtype
-    if out is None:
-        out = torch.empty(cfg.B, cfg.d_model, dtype=dt, device=dev)
-    for name, q, k, n in (("w_down", w_down, cfg.d_model, cfg.n_lat), ("w_out", w_out, cfg.e_q, cfg.d_model)):
-        if (q.K, q.N) != (k, n) or q.codes.device != dev:
-            raise ValueError(f"{name}: of (K, N) = {(q.K, q.N)} on {q.codes.device}, expected {(k, n)} on {dev}")
-    ring = (cfg.B, state.lat_ring.shape[1], cfg.n_lat)
-    if ring[1] != cca_decode_workspace_size(cfg)[1]:
-        raise ValueError(f"lat_ring: {ring[1]} rows, expected {cca_decode_workspace_size(cfg)[1]}")
-    x_shape = (cfg.B, cfg.d_model)
-    cc, cw = cfg.c(), w.c()
-    _mx_call("cca_decode_step_mx", dev, C.byref(cc), C.byref(cw), C.byref(w_down._c), C.byref(w_out._c), _mx_arg("x_new", x_new, x_shape, dt, dev),
-             state.cache._for(cfg), _mx_arg("lat_ring", state.lat_ring, ring, dt, dev), _mx_rows_arg("pos", pos, cfg, dev),
-             _mx_rows_arg("lens", lens, cfg, dev), max_len, _mx_arg("out", out, x_shape, dt, dev),
-             _mx_arg("workspace", state.workspace, state.workspace.shape, torch.uint8, dev), state.workspace.numel())
+    index, dt, B, E = state.cache._index, cfg.torch_dtype, cfg.B, cfg.d_model
+    x_shape, per_seq, ws = (B, E), (B,), state.workspace
+    out = torch.empty(x_shape, dtype=dt, device=state.cache._device) if out is None else out
+    for name, q, k, n in (("w_down", w_down, E, cfg.n_lat), ("w_out", w_out, cfg.e_q, E)):
+        if q.K != k or q.N != n or q._index != index:
+            raise ValueError(f"{name}: of (K, N) = {(q.K, q.N)} on {q.codes.device}, expected {(k, n)} on {state.cache._device}")
+    cw, ring = w.c(), (B, cfg.ring_rows(), cfg.n_lat)
+    _mx_call("cca_decode_step_mx", index, cfg.ref(), C.byref(cw), w_down._ref, w_out._ref, _mx_ptr("x_new", x_new, x_shape, dt, index),
+             state.cache._for(cfg), _mx_ptr("lat_ring", state.lat_ring, ring, dt, index), _mx_ptr("pos", pos, per_seq, torch.int32, index),
+             _mx_ptr("lens", lens, per_seq, torch.int32, index), max_len, _mx_ptr("out", out, x_shape, dt, index),
+             _mx_ptr("workspace", ws, ws.shape, torch.uint8, index), ws.numel())
     return out
 
 

@@ -12,8 +12,6 @@ namespace cca {
 
 namespace {
 
-constexpr int WAVES = 4;
-
 struct AttnArgs {
   int B, T, Hq, Hk, R, max_len, extra, nsplit, per, r0;
   float c;         // scale * log2(e)
@@ -21,11 +19,30 @@ struct AttnArgs {
   const void *q;
   bool q_f32;  // q holds fp32 (of the storage type's values)
   const unsigned char *k_codes, *k_scales, *v_codes, *v_scales;
-  float *part;    // (B, H_q, nsplit, 2 + d_h): m, l, o of a split (nsplit > 1)
+  mx_f2 *state;   // (B, H_q, nsplit): m, l of a split (nsplit > 1)
+  float *part;    // (B, H_q, nsplit, d_h): its o
   float *scores;  // (B, H_q, T) in log2 units, or null
   void *o;
   float *lse;
+  const float *weight_in;  // may be null: zeros
+  float *weight_out;
 };
+
+// 2^(m - M) for a part's maximum m and sum l; a part without rows has none
+__device__ __forceinline__ float rescale(float m, float l, float M) { return m == -INFINITY && l == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - M); }
+
+// weight_out[row ... row + 3] of a head = weight_in + sum, below len (the new rows of a step start from 0)
+__device__ __forceinline__ void add_weights(const AttnArgs &a, long long head, int row, int len, mx_f4 sum) {
+  const long long at = head * a.T + row;
+  if (row + 4 <= len - a.extra) {
+    if (a.weight_in) sum += *reinterpret_cast<const mx_f4 *>(a.weight_in + at);
+    *reinterpret_cast<mx_f4 *>(a.weight_out + at) = sum;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (row + i < len) a.weight_out[at + i] = (a.weight_in && row + i < len - a.extra ? a.weight_in[at + i] : 0.f) + sum[i];
+}
 
 __device__ __forceinline__ int seq_len(const AttnArgs &a, int b) { return mx_clamp(a.len[b], 0, a.max_len) + a.extra; }
 
@@ -52,10 +69,12 @@ struct Form {
   static constexpr int NG = N32 == 1 || N32 == 2 || N32 == 4 ? 1 : N32 == 8 ? 2 : (N32 + 2) / 4 + 1;  // groups that a lane's K channels touch
   static constexpr int COLS = TERMS == 1 ? 8 : 16;                // heads of a pass
   static constexpr int STRIDE = DH + 4;                           // floats of a head in the merge area: m, l, -, -, o
+  static constexpr int MANY = N32 <= 2 && TERMS < 3 ? 16 : 8;     // wavefronts of a workgroup that has its head to itself
+  static constexpr int RESIDENT = N32 <= 2 ? 4 : N32 <= 4 && TERMS < 3 ? 3 : 2;  // wavefronts of a SIMD that the registers are held to
 };
 
-template <int N32, int TERMS>
-__global__ __launch_bounds__(WAVES * 64) void mx_attn_kernel(AttnArgs a) {
+template <int N32, int TERMS, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, (WAVES == 4 ? Form<N32, TERMS>::RESIDENT : 1)) void mx_attn_kernel(AttnArgs a) {
   typedef Form<N32, TERMS> F;
   constexpr int DH = F::DH, NT = F::NT, BLK = F::BLK, PB = F::PB, NP = F::NP, VT = F::VT, NG = F::NG;
   extern __shared__ __attribute__((aligned(16))) float mrg[];  // [WAVES][COLS][STRIDE]
@@ -311,15 +330,15 @@ __global__ __launch_bounds__(WAVES * 64) void mx_attn_kernel(AttnArgs a) {
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
       const float *src = mrg + (w * F::COLS + r) * F::STRIDE;
-      const float f = src[0] == -INFINITY && src[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(src[0] - M);
+      const float f = rescale(src[0], src[1], M);
       L = fmaf(src[1], f, L);
       acc = fmaf(src[4 + ch], f, acc);
     }
     const long long h = (long long)b * a.Hq + g * a.R + a.r0 + r;
-    if (a.part) {
-      float *out = a.part + (h * a.nsplit + split) * (2 + DH);
-      if (ch == 0) out[0] = M, out[1] = L;
-      out[2 + ch] = acc;
+    if (a.state) {
+      const long long at = h * a.nsplit + split;
+      if (ch == 0) a.state[at] = mx_f2{M, L};
+      a.part[at * DH + ch] = acc;
     } else {
       const float res = L == 0.f ? 0.f : acc / L;
       if constexpr (TERMS == 3) static_cast<float *>(a.o)[h * DH + ch] = res;
@@ -329,148 +348,168 @@ __global__ __launch_bounds__(WAVES * 64) void mx_attn_kernel(AttnArgs a) {
   }
 }
 
-// The splits of a (sequence, query head) joined: o = sum o_s 2^(m_s - M) / sum l_s 2^(m_s - M), in index order.
-template <typename T>
-__global__ __launch_bounds__(256) void mx_combine_kernel(AttnArgs a, int dh) {
-  __shared__ float f[256];
-  __shared__ float red[8];
-  const int tid = threadIdx.x, stride = 2 + dh, lane = tid & 63, wave = tid >> 6;
-  for (long long bh = blockIdx.x; bh < (long long)a.B * a.Hq; bh += gridDim.x, __syncthreads()) {
-    const int len = seq_len(a, (int)(bh / a.Hq)), n = max(1, min(a.nsplit, (len + a.per - 1) / a.per));  // (nsplit <= 256)
-    const float *src = a.part + bh * a.nsplit * stride;
-    const float ms = tid < n ? src[(long long)tid * stride] : -INFINITY, ls = tid < n ? src[(long long)tid * stride + 1] : 0.f;
-    float M = ms;
-    for (int off = 32; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
-    if (lane == 0) red[wave] = M;
-    __syncthreads();
-    M = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    const float w = ms == -INFINITY && ls == 0.f ? 0.f : __builtin_amdgcn_exp2f(ms - M);
-    float L = ls * w;
-    for (int off = 32; off > 0; off >>= 1) L += __shfl_xor(L, off);
-    if (lane == 0) red[4 + wave] = L;
-    f[tid] = w;
-    __syncthreads();
-    L = (red[4] + red[5]) + (red[6] + red[7]);
-    if (tid < dh) {
-      float acc = 0.f;
-      for (int s = 0; s < n; ++s) acc = fmaf(src[(long long)s * stride + 2 + tid], f[s], acc);
-      store_f(static_cast<T *>(a.o) + bh * dh + tid, L == 0.f ? 0.f : acc / L);
-    }
-    if (tid == 0 && a.lse) a.lse[bh] = (M + log2f(L)) * 0.69314718055994530942f;
-  }
-}
-
-// weight_out[row] = weight_in[row] + sum over the R query heads of 2^(score - M) / L, four rows a thread; M and L from the splits' states.
+// ---------------------------------------------------------------------------
+// What follows the splits, in one launch.  The first workgroups join them: o = sum o_s 2^(m_s - M) / sum l_s 2^(m_s - M), 64 channels of a
+// query head each, a wavefront a quarter of the splits.  The others form the weights: weight_out[row] = weight_in[row] + sum over
+// the R query heads of 2^(score - M) / L, four rows a thread.
+// ---------------------------------------------------------------------------
 constexpr int W_ROWS = 1024, W_HEADS = 16;
-__global__ __launch_bounds__(256) void mx_weight_kernel(AttnArgs a, int dh, int tiles, const float *weight_in, float *weight_out, int fresh) {
-  __shared__ float top[W_HEADS], inv[W_HEADS];
-  const int tid = threadIdx.x, stride = 2 + dh, lane = tid & 63, wave = tid >> 6;
-  for (long long tile = blockIdx.x; tile < (long long)a.B * a.Hk * tiles; tile += gridDim.x) {
-  const long long head = tile / tiles;
-  const int b = (int)(head / a.Hk), g = (int)(head % a.Hk), len = seq_len(a, b), row = (int)(tile % tiles) * W_ROWS + 4 * tid;
-  if (row - 4 * tid >= len) continue;
-  const int n = min(a.nsplit, (len + a.per - 1) / a.per);
-  mx_f4 sum = {0.f, 0.f, 0.f, 0.f};
-  for (int r0 = 0; r0 < a.R; r0 += W_HEADS) {
-    __syncthreads();
-    for (int r = wave; r < min(W_HEADS, a.R - r0); r += 4) {
-      const float *src = a.part + ((long long)b * a.Hq + g * a.R + r0 + r) * a.nsplit * stride;
-      float M = -INFINITY, L = 0.f;
-      for (int s = lane; s < n; s += 64) M = fmaxf(M, src[(long long)s * stride]);
-      for (int off = 32; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
-      for (int s = lane; s < n; s += 64) {
-        const float ms = src[(long long)s * stride], ls = src[(long long)s * stride + 1];
-        L += ms == -INFINITY && ls == 0.f ? 0.f : ls * __builtin_amdgcn_exp2f(ms - M);
-      }
-      for (int off = 32; off > 0; off >>= 1) L += __shfl_xor(L, off);
-      if (lane == 0) top[r] = M, inv[r] = 1.f / L;
-    }
-    __syncthreads();
-    if (row < len)
-      for (int r = 0; r < min(W_HEADS, a.R - r0); ++r) {
-        const mx_f4 s = *reinterpret_cast<const mx_f4 *>(a.scores + ((long long)b * a.Hq + g * a.R + r0 + r) * a.T + row);
+// m and l of a head over its n <= 256 splits, by a wavefront
+__device__ __forceinline__ mx_f2 joined(const mx_f2 *state, int n, int lane, mx_f2 (&st)[4]) {
+  float M = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i] = fmaf(__builtin_amdgcn_exp2f(s[i] - top[r]), inv[r], sum[i]);
-      }
+  for (int i = 0; i < 4; ++i) {
+    st[i] = state[min(64 * i + lane, n - 1)];
+    if (64 * i + lane >= n) st[i] = mx_f2{-INFINITY, 0.f};
+    M = fmaxf(M, st[i][0]);
   }
-  const long long at = head * a.T + row;
+  for (int off = 32; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
+  float L = 0.f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (row + i < len) weight_out[at + i] = (weight_in && row + i < len - fresh ? weight_in[at + i] : 0.f) + sum[i];
+  for (int i = 0; i < 4; ++i) L += st[i][1] * rescale(st[i][0], st[i][1], M);
+  for (int off = 32; off > 0; off >>= 1) L += __shfl_xor(L, off);
+  return mx_f2{M, L};
+}
+template <typename T>
+__global__ __launch_bounds__(256) void mx_finish_kernel(AttnArgs a, int dh, long long joins, int tiles) {
+  __shared__ float f[256], acc[4][64], top[W_HEADS], inv[W_HEADS];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  for (long long item = blockIdx.x; item < joins + (long long)a.B * a.Hk * tiles; item += gridDim.x, __syncthreads()) {
+    mx_f2 st[4];
+    if (item < joins) {
+      const int chunks = (dh + 63) / 64, c0 = (int)(item % chunks) * 64;
+      const long long bh = item / chunks;
+      const int len = seq_len(a, (int)(bh / a.Hq)), n = max(1, min(a.nsplit, (len + a.per - 1) / a.per));
+      const mx_f2 ml = joined(a.state + bh * a.nsplit, n, lane, st);  // every wavefront for itself
+      const mx_f2 mine = wave == 0 ? st[0] : wave == 1 ? st[1] : wave == 2 ? st[2] : st[3];
+      f[tid] = rescale(mine[0], mine[1], ml[0]);  // of split `tid`
+      __syncthreads();
+      const int q = (n + 3) / 4, s0 = wave * q, s1 = min(n, s0 + q), ch = min(c0 + lane, dh - 1);
+      const float *src = a.part + bh * a.nsplit * dh + ch;
+      float sum = 0.f;
+      for (int s = s0; s < s1; s += 16) {
+        float v[16];
+#pragma unroll
+        for (int u = 0; u < 16; ++u) v[u] = src[(long long)min(s + u, s1 - 1) * dh];
+#pragma unroll
+        for (int u = 0; u < 16; ++u) sum = s + u < s1 ? fmaf(v[u], f[s + u], sum) : sum;
+      }
+      acc[wave][lane] = sum;
+      __syncthreads();
+      if (wave == 0) {
+        const float all = (acc[0][lane] + acc[1][lane]) + (acc[2][lane] + acc[3][lane]);
+        if (c0 + lane < dh) store_f(static_cast<T *>(a.o) + bh * dh + c0 + lane, ml[1] == 0.f ? 0.f : all / ml[1]);
+        if (c0 == 0 && lane == 0 && a.lse) a.lse[bh] = (ml[0] + log2f(ml[1])) * 0.69314718055994530942f;
+      }
+      continue;
+    }
+    const long long head = (item - joins) / tiles;
+    const int b = (int)(head / a.Hk), g = (int)(head % a.Hk), len = seq_len(a, b), row0 = (int)((item - joins) % tiles) * W_ROWS, row = row0 + 4 * tid;
+    if (row0 >= len) continue;
+    const int n = min(a.nsplit, (len + a.per - 1) / a.per);
+    mx_f4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int r0 = 0; r0 < a.R; r0 += W_HEADS) {
+      const int nr = min(W_HEADS, a.R - r0);
+      const long long h0 = (long long)b * a.Hq + g * a.R + r0;
+      if (r0) __syncthreads();
+      for (int r = wave; r < nr; r += 4) {
+        const mx_f2 ml = joined(a.state + (h0 + r) * a.nsplit, n, lane, st);
+        if (lane == 0) top[r] = ml[0] == -INFINITY ? 0.f : ml[0], inv[r] = ml[1] == 0.f ? 0.f : 1.f / ml[1];
+      }
+      __syncthreads();
+      if (row < len) {
+        const float *sc = a.scores + h0 * a.T + row;
+        for (int r = 0; r < nr; r += 4) {
+          mx_f4 s[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) s[u] = *reinterpret_cast<const mx_f4 *>(sc + (long long)min(r + u, nr - 1) * a.T);
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            if (r + u < nr) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) sum[i] = fmaf(__builtin_amdgcn_exp2f(s[u][i] - top[r + u]), inv[r + u], sum[i]);
+            }
+        }
+      }
+    }
+    add_weights(a, head, row, len, sum);
   }
 }
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
-template <int N32, int TERMS>
-hipError_t launch(const AttnArgs &a, hipStream_t s) {
+template <int N32, int TERMS, int WAVES>
+hipError_t launch_waves(const AttnArgs &a, hipStream_t s) {
   typedef Form<N32, TERMS> F;
   constexpr size_t lds = sizeof(float) * WAVES * F::COLS * F::STRIDE;
-  if (hipError_t e = raise_lds_limit<mx_attn_kernel<N32, TERMS>>(lds); e != hipSuccess) return e;
-  mx_attn_kernel<N32, TERMS><<<(unsigned)((long long)a.B * a.Hk * a.nsplit), WAVES * 64, lds, s>>>(a);
+  if (hipError_t e = raise_lds_limit<mx_attn_kernel<N32, TERMS, WAVES>>(lds); e != hipSuccess) return e;
+  mx_attn_kernel<N32, TERMS, WAVES><<<(unsigned)((long long)a.B * a.Hk * a.nsplit), WAVES * 64, lds, s>>>(a);
   return hipGetLastError();
 }
+template <int N32, int TERMS>
+hipError_t launch(const AttnArgs &a, bool many, hipStream_t s) {
+  return many ? launch_waves<N32, TERMS, Form<N32, TERMS>::MANY>(a, s) : launch_waves<N32, TERMS, 4>(a, s);
+}
 template <int TERMS>
-hipError_t launch_width(int n32, const AttnArgs &a, hipStream_t s) {
+hipError_t launch_width(int n32, const AttnArgs &a, bool many, hipStream_t s) {
   switch (n32) {
-    case 1: return launch<1, TERMS>(a, s);
-    case 2: return launch<2, TERMS>(a, s);
-    case 3: return launch<3, TERMS>(a, s);
-    case 4: return launch<4, TERMS>(a, s);
-    case 5: return launch<5, TERMS>(a, s);
-    case 6: return launch<6, TERMS>(a, s);
-    case 7: return launch<7, TERMS>(a, s);
-    default: return launch<8, TERMS>(a, s);
+    case 1: return launch<1, TERMS>(a, many, s);
+    case 2: return launch<2, TERMS>(a, many, s);
+    case 3: return launch<3, TERMS>(a, many, s);
+    case 4: return launch<4, TERMS>(a, many, s);
+    case 5: return launch<5, TERMS>(a, many, s);
+    case 6: return launch<6, TERMS>(a, many, s);
+    case 7: return launch<7, TERMS>(a, many, s);
+    default: return launch<8, TERMS>(a, many, s);
   }
+}
+
+struct Layout {
+  size_t state, part, scores, total;
+};
+Layout layout(const Dims &d) {
+  Layout L;
+  size_t off = 0;
+  auto take = [&](size_t n) { const size_t at = off; off += align256(n); return at; };
+  const size_t splits = (size_t)d.B * d.Hq * mx_max_splits((long long)d.B * d.Hk, d.T);
+  L.state = take(splits * sizeof(mx_f2));
+  L.part = take(splits * d.dh * sizeof(float));
+  L.scores = take((size_t)d.B * d.Hq * d.T * sizeof(float));
+  L.total = off;
+  return L;
 }
 
 }  // namespace
 
-struct MxAttnLayout {
-  size_t part, scores, total;
-};
-static MxAttnLayout mx_attn_layout(const Dims &d) {
-  MxAttnLayout L;
-  L.part = 0;
-  L.scores = align256((size_t)d.B * d.Hq * mx_max_splits((long long)d.B * d.Hk, d.T) * (2 + d.dh) * sizeof(float));
-  L.total = L.scores + align256((size_t)d.B * d.Hq * d.T * sizeof(float));
-  return L;
-}
-size_t mx_attention_scratch_bytes(const Dims &d) { return mx_attn_layout(d).total; }
+size_t mx_attention_scratch_bytes(const Dims &d) { return layout(d).total; }
 
 hipError_t mx_attention(const Dims &d, const cca_mx_cache &c, const void *q, bool q_f32, const int *len, int max_len, int extra, void *o,
                         float *lse, const float *weight_in, float *weight_out, void *workspace, hipStream_t s) {
-  const MxAttnLayout L = mx_attn_layout(d);
+  const Layout L = layout(d);
   unsigned char *ws = static_cast<unsigned char *>(workspace);
   const int longest = max_len + extra;
-  const int per = mx_rows_per_split((long long)d.B * d.Hk, d.T, longest, d.dh), nsplit = longest > per ? (longest + per - 1) / per : 1;
+  const long long groups = (long long)d.B * d.Hk;
+  const MxSplit split = mx_split(groups, d.T, longest, d.dh);
+  const bool finish = split.n > 1 || weight_out;
   auto p = [](const void *x) { return static_cast<const unsigned char *>(x); };
-  AttnArgs a{d.B, d.T, d.Hq, d.Hk, d.R, max_len, extra, nsplit, per, 0, d.scale * 1.44269504088896340736f, len, q, q_f32 || !d.bf16,
-             p(c.k_codes), p(c.k_scales), p(c.v_codes), p(c.v_scales),
-             nsplit > 1 || weight_out ? reinterpret_cast<float *>(ws + L.part) : nullptr,
-             weight_out ? reinterpret_cast<float *>(ws + L.scores) : nullptr, o, lse};
+  AttnArgs a{d.B, d.T, d.Hq, d.Hk, d.R, max_len, extra, split.n, split.rows, 0, d.scale * 1.44269504088896340736f, len, q, q_f32 || !d.bf16,
+             p(c.k_codes), p(c.k_scales), p(c.v_codes), p(c.v_scales), finish ? reinterpret_cast<mx_f2 *>(ws + L.state) : nullptr,
+             reinterpret_cast<float *>(ws + L.part), weight_out ? reinterpret_cast<float *>(ws + L.scores) : nullptr, o, lse, weight_in, weight_out};
   hipError_t e;
   for (; a.r0 < d.R;) {
     const int left = d.R - a.r0;
-    if (!d.bf16) e = launch_width<3>(d.dh / 32, a, s), a.r0 += 16;
-    else if (left <= 8) e = launch_width<1>(d.dh / 32, a, s), a.r0 += 8;
-    else e = launch_width<2>(d.dh / 32, a, s), a.r0 += 16;
+    if (!d.bf16) e = launch_width<3>(d.dh / 32, a, split.many, s), a.r0 += 16;
+    else if (left <= 8) e = launch_width<1>(d.dh / 32, a, split.many, s), a.r0 += 8;
+    else e = launch_width<2>(d.dh / 32, a, split.many, s), a.r0 += 16;
     if (e != hipSuccess) return e;
   }
-  if (a.part) {
-    const long long heads = (long long)d.B * d.Hq;
-    const unsigned grid = (unsigned)(heads < (1 << 20) ? heads : 1 << 20);
-    if (d.bf16) mx_combine_kernel<bf16_t><<<grid, 256, 0, s>>>(a, d.dh);
-    else mx_combine_kernel<float><<<grid, 256, 0, s>>>(a, d.dh);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
-  if (weight_out && longest > 0) {
-    const int tiles = (longest + W_ROWS - 1) / W_ROWS;
-    const long long all = (long long)d.B * d.Hk * tiles;
-    mx_weight_kernel<<<(unsigned)(all < (1 << 20) ? all : 1 << 20), 256, 0, s>>>(a, d.dh, tiles, weight_in, weight_out, extra);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
-  return hipSuccess;
+  if (!finish) return hipSuccess;
+  const int tiles = weight_out ? (longest + W_ROWS - 1) / W_ROWS : 0;
+  const long long joins = (long long)d.B * d.Hq * ((d.dh + 63) / 64), items = joins + groups * tiles;
+  const unsigned grid = (unsigned)(items < (1 << 20) ? items : 1 << 20);
+  if (d.bf16) mx_finish_kernel<bf16_t><<<grid, 256, 0, s>>>(a, d.dh, joins, tiles);
+  else mx_finish_kernel<float><<<grid, 256, 0, s>>>(a, d.dh, joins, tiles);
+  return hipGetLastError();
 }
 
 }  // namespace cca

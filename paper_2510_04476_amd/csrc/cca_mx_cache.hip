@@ -122,12 +122,14 @@ __global__ __launch_bounds__(256) void mx_rows_kernel(StoreArgs a, T *__restrict
 // ---------------------------------------------------------------------------
 // Eviction, first launch: one workgroup per (sequence, head) picks the rows that stay.  A row's rank as an unsigned key: recent
 // rows 0xffffffff, else the weight's bits turned so that they order as the numbers do, NaN 0.  The key of the last row that stays is
-// found digit by digit (11 + 11 + 10 bits): a histogram in LDS of the rows that agree with the digits so far.  Rows
-// above it stay, and of those that equal it the first.  One ordered sum over the rows then numbers the holes below `budget`
-// and the kept rows beyond it.
-// Out: kept rows in row order (`list`, budget entries, those from hole 0's counterpart on are the movers) and holes; counts.
+// found digit by digit (11 + 11 + 10 bits): a histogram in LDS of the rows that agree with the digits so far, two copies side by
+// side (neighbouring lanes hold similar weights: one copy has them queue for the same words).  Rows above that key stay, and of
+// those that equal it the first.  Then each wavefront counts both kinds in its own stretch of rows and, behind one sum over the
+// wavefronts, numbers the holes below `budget` and the kept rows beyond it.
+// HELD: the keys lie in LDS, so that weights and positions are read once; longer heads are read again by every pass.
 // ---------------------------------------------------------------------------
-constexpr int SEL = 1024, DIGIT = 11;
+constexpr int SEL = 1024, DIGIT = 11, COPIES = 2;
+constexpr int HELD_ROWS = 32768;  // 128 KB of keys beside 16 KB of histogram
 struct EvictArgs {
   long long heads;  // B * H_k
   int Hk, T, dh, max_len, budget, recent;
@@ -139,145 +141,241 @@ struct EvictArgs {
   int *holes, *movers, *counts;  // (B * Hk, half), (B * Hk, half), (B * Hk, 2): number of moves, new length
   int half;                      // min(budget, T - budget): the most moves
 };
+typedef int mx_i4 __attribute__((ext_vector_type(4)));
 
-__device__ __forceinline__ uint32_t rank_key(float w, int pos, int newest, int recent) {
-  if ((long long)pos > (long long)newest - recent) return 0xffffffffu;
-  if (w != w) return 0u;
-  const uint32_t u = __float_as_uint(w + 0.f);  // -0 counts as 0
-  return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+__device__ __forceinline__ uint32_t rank_key(float w, int pos, long long old) {
+  const uint32_t u = __float_as_uint(w + 0.f), k = (u & 0x80000000u) ? ~u : u | 0x80000000u;  // -0 counts as 0
+  return (long long)pos > old ? 0xffffffffu : w != w ? 0u : k;
 }
-
-__device__ __forceinline__ int block_max(int v, int *red) {
-  for (int off = 32; off > 0; off >>= 1) v = max(v, __shfl_xor(v, off));
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = red[0];
-  for (int w = 1; w < SEL / 64; ++w) v = max(v, red[w]);
-  __syncthreads();
-  return v;
+// Sum over the lanes up to this one: shifts inside each row of 16 lanes, then the rows' last sums handed on
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr 1, 2, 4, 8 (zero from before the row)
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast 15 into rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast 31 into rows 2 and 3
+  return x;
 }
-
+template <bool HELD>
 __global__ __launch_bounds__(SEL) void mx_select_kernel(EvictArgs a) {
-  __shared__ int hist[1 << DIGIT];
-  __shared__ int red[SEL / 64][2];
-  __shared__ int found[2];
+  extern __shared__ __attribute__((aligned(16))) int sel_lds[];
+  int *const hist = sel_lds;                                                        // [bin][copy]
+  uint32_t *const keys = reinterpret_cast<uint32_t *>(sel_lds + (COPIES << DIGIT));  // HELD: of every row
+  __shared__ int red[SEL / 64][2], found[2];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   for (long long head = blockIdx.x; head < a.heads; head += gridDim.x, __syncthreads()) {
-  const int n = mx_clamp(a.len[head / a.Hk], 0, a.max_len);
-  const float *w = a.weight + head * a.T;
-  const int *p = a.pos + head * a.T;
-  const bool apart = a.weight_out != a.weight || a.pos_out != a.pos;
-  int *counts = a.counts + head * 2;
-  if (n <= a.budget) {
-    if (tid == 0) counts[0] = 0, counts[1] = n;
-    if (apart)
-      for (int i = tid; i < n; i += SEL) a.weight_out[head * a.T + i] = w[i], a.pos_out[head * a.T + i] = p[i];
-    continue;
-  }
-  int newest = INT32_MIN;
-  for (int i = tid; i < n; i += SEL) newest = max(newest, p[i]);
-  newest = block_max(newest, &red[0][0]);
-  // the budget-th largest key
-  uint32_t prefix = 0, mask = 0;
-  int want = a.budget;  // how many of the rows that agree with the prefix are still to be taken
-  for (int pass = 0; pass < 3; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-    for (int i = tid; i < (1 << DIGIT); i += SEL) hist[i] = 0;
-    __syncthreads();
-    for (int i = tid; i < n; i += SEL) {
-      const uint32_t key = rank_key(w[i], p[i], newest, a.recent);
-      if ((key & mask) == prefix) atomicAdd(&hist[(key >> shift) & ((1u << bits) - 1u)], 1);
+    const float *const w = a.weight + head * a.T;
+    const int *const p = a.pos + head * a.T;
+    const bool apart = a.weight_out != a.weight || a.pos_out != a.pos;
+    float *const wo = a.weight_out + head * a.T;
+    int *const po = a.pos_out + head * a.T;
+    const int n = mx_clamp(a.len[head / a.Hk], 0, a.max_len);
+    if (tid == 0) a.counts[head * 2 + 1] = min(n, a.budget);
+    if (n <= a.budget) {
+      if (tid == 0) a.counts[head * 2] = 0;
+      if (apart)
+        for (int i = tid; i < n; i += SEL) wo[i] = w[i], po[i] = p[i];
+      continue;
     }
-    __syncthreads();
-    // from the top: thread t holds two neighbouring bins; the first bin at which the sum reaches `want`
-    const int hi = (1 << DIGIT) - 1 - 2 * tid, c1 = hist[hi], c0 = hist[hi - 1];
-    int sum = c1 + c0;
-    for (int off = 1; off < 64; off <<= 1) {
-      const int up = __shfl_up(sum, off);
-      if (lane >= off) sum += up;
+    // Rows four at a time, four groups requested together; the capacity is a multiple of 32, so a group that begins below n is inside it.
+    // (Loops stay rolled: a launch runs them a few times, and code that it has to fetch first costs more than the iterations.  With the
+    // rows of 8 iterations unrolled into registers: 4608 and 30011 rows 17.6 and 38.6 us.)
+    auto groups = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll 1
+      for (int r0 = 4 * tid; r0 < n; r0 += 16 * SEL) {
+        mx_f4 wv[4];
+        mx_i4 pv[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int at = min(r0 + 4 * SEL * u, a.T - 4);
+          wv[u] = *reinterpret_cast<const mx_f4 *>(w + at);
+          pv[u] = *reinterpret_cast<const mx_i4 *>(p + at);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (r0 + 4 * SEL * u < n) f(r0 + 4 * SEL * u, wv[u], pv[u]);
+      }
+    };
+    int newest = INT32_MIN;
+#pragma unroll 1
+    for (int r0 = 4 * tid; r0 < n; r0 += 32 * SEL) {
+      mx_i4 pv[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) pv[u] = *reinterpret_cast<const mx_i4 *>(p + min(r0 + 4 * SEL * u, a.T - 4));
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) newest = r0 + 4 * SEL * u + e < n ? max(newest, pv[u][e]) : newest;
     }
-    if (lane == 63) red[wave][0] = sum;
+    for (int off = 32; off > 0; off >>= 1) newest = max(newest, __shfl_xor(newest, off));
+    if (lane == 0) red[wave][0] = newest;
+    for (int i = tid; i < (COPIES << DIGIT) / 4; i += SEL) reinterpret_cast<mx_i4 *>(hist)[i] = mx_i4{0, 0, 0, 0};
     __syncthreads();
-    int before = 0;
-    for (int x = 0; x < wave; ++x) before += red[x][0];
-    before += sum - (c1 + c0);
-    if (before < want && before + c1 >= want) found[0] = hi, found[1] = before;
-    else if (before + c1 < want && before + c1 + c0 >= want) found[0] = hi - 1, found[1] = before + c1;
-    __syncthreads();
-    prefix |= (uint32_t)found[0] << shift;
-    mask |= ((1u << bits) - 1u) << shift;
-    want -= found[1];
-    __syncthreads();
-  }
-  // `want` rows of key `prefix` stay, the first ones.  Thread t takes rows t * per ...: rows above the key and rows that equal it
-  // before its own, by one sum over the workgroup.
-  const int per = (n + SEL - 1) / SEL, i0 = min(n, tid * per), i1 = min(n, i0 + per);
-  int above = 0, equal = 0;
-  for (int i = i0; i < i1; ++i) {
-    const uint32_t key = rank_key(w[i], p[i], newest, a.recent);
-    above += key > prefix;
-    equal += key == prefix;
-  }
-  int sa = above, se = equal;
-  for (int off = 1; off < 64; off <<= 1) {
-    const int ua = __shfl_up(sa, off), ue = __shfl_up(se, off);
-    if (lane >= off) sa += ua, se += ue;
-  }
-  if (lane == 63) red[wave][0] = sa, red[wave][1] = se;
-  __syncthreads();
-  for (int x = 0; x < wave; ++x) sa += red[x][0], se += red[x][1];
-  sa -= above;
-  se -= equal;
-  int *holes = a.holes + head * a.half, *movers = a.movers + head * a.half;
-  for (int i = i0; i < i1; ++i) {
-    const float wi = w[i];
-    const int pi = p[i];
-    const uint32_t key = rank_key(wi, pi, newest, a.recent);
-    const int kept = sa + min(se, want);  // rows before i that stay
-    const bool keep = key > prefix || (key == prefix && se < want);
-    if (i < a.budget) {
-      if (!keep) holes[i - kept] = i;
-      else if (apart) a.weight_out[head * a.T + i] = wi, a.pos_out[head * a.T + i] = pi;
-    } else if (keep) {
-      movers[a.budget - 1 - kept] = i;  // counted from the last kept row: the list is filled backwards
+#pragma unroll
+    for (int x = 0; x < SEL / 64; ++x) newest = max(newest, red[x][0]);
+    const long long old = (long long)newest - a.recent;  // the largest position that is not recent
+    uint32_t prefix = 0, mask = 0;
+    int want = a.budget;  // how many of the rows that agree with the prefix are still to be taken
+#pragma unroll 1
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+      const uint32_t bins = pass == 2 ? 1023u : 2047u;
+      auto count = [&](int row, uint32_t k) __attribute__((always_inline)) {
+        if (row < n && (k & mask) == prefix) atomicAdd(&hist[((k >> shift) & bins) * COPIES + (lane & (COPIES - 1))], 1);
+      };
+      if (HELD && pass > 0) {
+#pragma unroll 1
+        for (int r = 4 * tid; r < n; r += 4 * SEL) {
+          const mx_u4 k = *reinterpret_cast<const mx_u4 *>(keys + r);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) count(r + e, k[e]);
+        }
+      } else {
+        groups([&](int row, mx_f4 wv, mx_i4 pv) __attribute__((always_inline)) {
+          mx_u4 k;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t ke = rank_key(wv[e], pv[e], old);
+            k[e] = ke;
+            count(row + e, ke);
+          }
+          if constexpr (HELD) *reinterpret_cast<mx_u4 *>(keys + row) = k;
+        });
+      }
+      __syncthreads();
+      // from the top: thread t holds two neighbouring bins, which it clears; the first bin at which the sum reaches `want`
+      const int hi = (1 << DIGIT) - 1 - 2 * tid;
+      int c[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        int2 *const h = reinterpret_cast<int2 *>(hist) + (hi - x);
+        const int2 v = *h;
+        *h = make_int2(0, 0);
+        c[x] = v.x + v.y;
+      }
+      const int sum = wave_scan(c[0] + c[1]);
+      if (lane == 63) red[wave][1] = sum;
+      __syncthreads();
+      int before = sum - c[0] - c[1];
+#pragma unroll
+      for (int x = 0; x < SEL / 64; ++x) before += x < wave ? red[x][1] : 0;
+      if (before < want && before + c[0] >= want) found[0] = hi, found[1] = before;
+      else if (before + c[0] < want && before + c[0] + c[1] >= want) found[0] = hi - 1, found[1] = before + c[0];
+      __syncthreads();
+      prefix |= (uint32_t)found[0] << shift;
+      mask |= bins << shift;
+      want -= found[1];
+      // (`found` and `red` are written again behind the next pass's barriers)
     }
-    sa += key > prefix;
-    se += key == prefix;
-    if (i == a.budget - 1) counts[0] = a.budget - (kept + (keep ? 1 : 0)), counts[1] = a.budget;
-  }
+    // `want` rows of key `prefix` stay, the first ones.  A wavefront's stretch: whole lines of 256 rows
+    const int stretch = ((n + SEL / 64 - 1) / (SEL / 64) + 255) / 256 * 256, r0 = wave * stretch, r1 = min(n, r0 + stretch);
+    // keys of rows `row` ... `row` + 3, this lane's (row is below n)
+    auto keys_at = [&](int row) __attribute__((always_inline)) {
+      if constexpr (HELD) return *reinterpret_cast<const mx_u4 *>(keys + row);
+      const mx_f4 wv = *reinterpret_cast<const mx_f4 *>(w + row);
+      const mx_i4 pv = *reinterpret_cast<const mx_i4 *>(p + row);
+      mx_u4 k;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) k[e] = rank_key(wv[e], pv[e], old);
+      return k;
+    };
+    auto counts_of = [&](int row, mx_u4 k) __attribute__((always_inline)) {  // above | equal << 16: at most 8192 rows of a stretch to a lane
+      int c = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) c += row + e < n ? k[e] > prefix ? 1 : k[e] == prefix ? 1 << 16 : 0 : 0;
+      return c;
+    };
+    int above = 0, equal = 0;
+#pragma unroll 1
+    for (int row = r0 + 4 * lane; row < r1; row += 256) {
+      const int c = counts_of(row, keys_at(row));
+      above += c & 0xffff;
+      equal += c >> 16;
+    }
+    for (int off = 32; off > 0; off >>= 1) above += __shfl_xor(above, off), equal += __shfl_xor(equal, off);
+    if (lane == 0) red[wave][0] = above, red[wave][1] = equal;
+    __syncthreads();
+    above = equal = 0;  // before this wavefront's rows
+#pragma unroll
+    for (int x = 0; x < SEL / 64; ++x) above += x < wave ? red[x][0] : 0, equal += x < wave ? red[x][1] : 0;
+    int *const holes = a.holes + head * a.half, *const movers = a.movers + head * a.half;
+#pragma unroll 1
+    for (int r = r0; r < r1; r += 256) {
+      const int row = r + 4 * lane;
+      mx_u4 k = {0u, 0u, 0u, 0u};
+      mx_f4 wv = {0.f, 0.f, 0.f, 0.f};
+      mx_i4 pv = {0, 0, 0, 0};
+      if (row < n) k = keys_at(row);
+      if (apart && row < a.budget) {
+        wv = *reinterpret_cast<const mx_f4 *>(w + row);
+        pv = *reinterpret_cast<const mx_i4 *>(p + row);
+      }
+      const int mine = row < n ? counts_of(row, k) : 0, upto = wave_scan(mine), all = __builtin_amdgcn_readlane(upto, 63);
+      int sa = above + ((upto - mine) & 0xffff), se = equal + ((upto - mine) >> 16);
+      above += all & 0xffff;
+      equal += all >> 16;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int i = row + e, kept = sa + min(se, want);  // rows before i that stay
+        const bool is_above = i < n && k[e] > prefix, is_equal = i < n && k[e] == prefix, keep = is_above || (is_equal && se < want);
+        if (i < a.budget) {
+          if (!keep) holes[i - kept] = i;
+          else if (apart) wo[i] = wv[e], po[i] = pv[e];
+        } else if (keep) {
+          movers[a.budget - 1 - kept] = i;  // counted from the last kept row: the list is filled backwards
+        }
+        if (i == a.budget - 1) a.counts[head * 2] = a.budget - (kept + (keep ? 1 : 0));
+        sa += is_above;
+        se += is_equal;
+      }
+    }
   }
 }
 
-// Second launch: hole h gets row movers[moves - 1 - h].  Sources lie at or beyond `budget`, targets below: no order is needed.  A
-// workgroup takes 32 moves of a head: a wavefront the codes of 8, then a thread a scale byte, a weight, a position.
-constexpr int MOVES = 32;
-__global__ __launch_bounds__(256) void mx_move_kernel(EvictArgs a, unsigned char *__restrict__ k_codes, unsigned char *__restrict__ k_scales,
-                                                     unsigned char *__restrict__ v_codes, unsigned char *__restrict__ v_scales) {
-  const int tid = threadIdx.x, per = a.half > MOVES ? (a.half + MOVES - 1) / MOVES : 1;
-  for (long long tile = blockIdx.x; tile < a.heads * per; tile += gridDim.x) {
-  const long long head = tile / per;
-  const int moves = a.counts[head * 2], m0 = (int)(tile % per) * MOVES;
-  if (m0 == 0 && tid == 0 && head % a.Hk == 0) a.len_out[head / a.Hk] = a.counts[head * 2 + 1];
-  if (m0 >= moves) continue;
-  const int nm = min(MOVES, moves - m0), words = a.dh / 8, groups = a.dh / 32;
-  const int *holes = a.holes + head * a.half + m0, *movers = a.movers + head * a.half + (moves - 1 - m0);
-  const long long base = head * a.T;
-  for (int i = tid; i < nm * words * 2; i += 256) {
-    const int m = i / (2 * words), c = i % (2 * words);
-    uint32_t *codes = reinterpret_cast<uint32_t *>(c < words ? k_codes : v_codes);
-    const int x = c < words ? c : c - words;
-    codes[(base + holes[m]) * words + x] = codes[(base + movers[-m]) * words + x];
-  }
-  for (int i = tid; i < nm * groups * 2; i += 256) {
-    const int m = i % nm, g = i / nm;
-    unsigned char *scales = (g < groups ? k_scales : v_scales) + (head * groups + (g < groups ? g : g - groups)) * a.T;
-    scales[holes[m]] = scales[movers[-m]];
-  }
-  if (tid < nm) {
-    const long long from = base + movers[-tid], to = base + holes[tid];
-    a.weight_out[to] = a.weight[from];
-    a.pos_out[to] = a.pos[from];
-  }
+// ---------------------------------------------------------------------------
+// Second launch: hole m gets row movers[moves - 1 - m].  Sources lie at or beyond `budget`, targets below: no order is needed.  A
+// workgroup takes 32 moves of a head: a word of codes, then a scale byte, a weight and a position to a thread in turn.  (Moved by the
+// workgroup that picked them, 512 of dh = 128 and 3300 of 64 took 8 and 31 us more; this launch takes 6.)
+// ---------------------------------------------------------------------------
+struct Cache {
+  unsigned char *k_codes, *k_scales, *v_codes, *v_scales;
+};
+constexpr int PART = 32;
+__global__ __launch_bounds__(256) void mx_move_kernel(EvictArgs a, Cache c) {
+  const int tid = threadIdx.x, per = a.half > PART ? (a.half + PART - 1) / PART : 1;
+  const int words = a.dh / 8, groups = a.dh / 32;  // words of a row's codes; scale bytes
+  __shared__ int from[PART], to[PART];
+  for (long long tile = blockIdx.x; tile < a.heads * per; tile += gridDim.x, __syncthreads()) {
+    const long long head = tile / per, base = head * a.T;
+    const int moves = a.counts[head * 2], m0 = (int)(tile % per) * PART, nm = min(PART, moves - m0);
+    if (m0 == 0 && tid == 0 && head % a.Hk == 0) a.len_out[head / a.Hk] = a.counts[head * 2 + 1];
+    if (nm <= 0) continue;
+    if (tid < nm) {
+      const int f = a.movers[head * a.half + moves - 1 - m0 - tid], t = a.holes[head * a.half + m0 + tid];
+      from[tid] = f, to[tid] = t;
+      a.weight_out[base + t] = a.weight[base + f];
+      a.pos_out[base + t] = a.pos[base + f];
+    }
+    __syncthreads();
+    // eight threads to a row's codes of K and of V each
+    const int m = tid >> 3;
+    if (m < nm) {
+      const long long f = (base + from[m]) * words, t = (base + to[m]) * words;
+#pragma unroll 4
+      for (int x = tid & 7; x < words; x += 8) {
+        const uint32_t k = reinterpret_cast<const uint32_t *>(c.k_codes)[f + x], v = reinterpret_cast<const uint32_t *>(c.v_codes)[f + x];
+        reinterpret_cast<uint32_t *>(c.k_codes)[t + x] = k;
+        reinterpret_cast<uint32_t *>(c.v_codes)[t + x] = v;
+      }
+      // and to its scale bytes, T bytes apart
+      if ((tid & 7) < groups) {
+        const long long at = (head * groups + (tid & 7)) * a.T;
+        const unsigned char k = c.k_scales[at + from[m]], v = c.v_scales[at + from[m]];
+        c.k_scales[at + to[m]] = k;
+        c.v_scales[at + to[m]] = v;
+      }
+    }
   }
 }
 
@@ -306,27 +404,35 @@ hipError_t mx_rows(const Dims &d, const cca_mx_cache &c, void *k, void *v, int n
   return hipGetLastError();
 }
 
-// The plan of an eviction: holes, movers, counts.  A budget leaves at most T / 2 moves.
+// The plan of an eviction: holes, movers (a budget leaves at most T / 2 moves), counts.
 size_t mx_evict_scratch_bytes(const Dims &d) {
   const size_t heads = (size_t)d.B * d.Hk;
   return 2 * align256(heads * ((size_t)d.T / 2) * sizeof(int)) + align256(heads * 2 * sizeof(int));
 }
 
-hipError_t mx_evict(const Dims &d, const cca_mx_cache &c, int *len, int max_len, int budget, int recent, float *weight_out, int *pos_out,
+hipError_t mx_evict(const Dims &d, const cca_mx_cache &cache, int *len, int max_len, int budget, int recent, float *weight_out, int *pos_out,
                     int *len_out, void *workspace, hipStream_t s) {
-  const size_t heads = (size_t)d.B * d.Hk;
+  const size_t heads = (size_t)d.B * d.Hk, list = align256(heads * ((size_t)d.T / 2) * sizeof(int));
   unsigned char *ws = static_cast<unsigned char *>(workspace);
-  const size_t list = align256(heads * ((size_t)d.T / 2) * sizeof(int));
-  const int half = budget < max_len - budget ? budget : max_len - budget;  // (max_len <= T: at most T / 2)
-  EvictArgs a{(long long)heads, d.Hk, d.T, d.dh, max_len, budget, recent, len, c.weight, reinterpret_cast<const int *>(c.pos),
-              weight_out ? weight_out : c.weight, pos_out ? pos_out : reinterpret_cast<int *>(c.pos), len_out ? len_out : len,
-              reinterpret_cast<int *>(ws), reinterpret_cast<int *>(ws + list), reinterpret_cast<int *>(ws + 2 * list), half > 0 ? half : 0};
-  mx_select_kernel<<<(unsigned)(a.heads < MAX_GRID ? a.heads : MAX_GRID), SEL, 0, s>>>(a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const long long tiles = a.heads * (a.half > MOVES ? (a.half + MOVES - 1) / MOVES : 1);
-  auto p = [](void *x) { return static_cast<unsigned char *>(x); };
-  mx_move_kernel<<<(unsigned)(tiles < MAX_GRID ? tiles : MAX_GRID), 256, 0, s>>>(a, p(c.k_codes), p(c.k_scales), p(c.v_codes), p(c.v_scales));
+  auto ints = [](unsigned char *p) { return reinterpret_cast<int *>(p); };
+  auto bytes = [](void *p) { return static_cast<unsigned char *>(p); };
+  int *const pos = reinterpret_cast<int *>(cache.pos);
+  const int most = budget < max_len - budget ? budget : max_len - budget;  // (max_len <= T: at most T / 2)
+  const EvictArgs a{(long long)heads, d.Hk, d.T, d.dh, max_len, budget, recent, len, cache.weight, pos, weight_out ? weight_out : cache.weight,
+                    pos_out ? pos_out : pos, len_out ? len_out : len, ints(ws), ints(ws + list), ints(ws + 2 * list), most > 0 ? most : 0};
+  const unsigned grid = (unsigned)(a.heads < MAX_GRID ? a.heads : MAX_GRID);
+  constexpr size_t HIST = (size_t)(COPIES << DIGIT) * 4;
+  hipError_t e;
+  if (max_len <= HELD_ROWS) {
+    if ((e = raise_lds_limit<mx_select_kernel<true>>(HIST + (size_t)HELD_ROWS * 4)) != hipSuccess) return e;
+    mx_select_kernel<true><<<grid, SEL, HIST + (size_t)(max_len + 3) / 4 * 16, s>>>(a);
+  } else {
+    mx_select_kernel<false><<<grid, SEL, HIST, s>>>(a);
+  }
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  const long long tiles = a.heads * (a.half > PART ? (a.half + PART - 1) / PART : 1);
+  mx_move_kernel<<<(unsigned)(tiles < MAX_GRID ? tiles : MAX_GRID), 256, 0, s>>>(
+      a, Cache{bytes(cache.k_codes), bytes(cache.k_scales), bytes(cache.v_codes), bytes(cache.v_scales)});
   return hipGetLastError();
 }
 

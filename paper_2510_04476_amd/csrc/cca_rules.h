@@ -462,17 +462,25 @@ constexpr size_t decode_up_lds(long long B, int e_q) { return (size_t)((e_q + 12
 constexpr size_t DECODE_UP_LDS = decode_up_lds(1, UP_CHANNELS);
 
 // ---- attention over the 4-bit cache: rows of a split ----------------------------------------------------------------------
-// Every split but a sequence's last holds this many rows: whole rounds of the kernel's four wavefronts (64 rows each, 32 above d_h =
-// 128), as few splits as leave about 1024 workgroups on the chip.  groups = sequences x KV heads.
+// groups = sequences x KV heads.  Short rows of few groups: one workgroup of 16 (8) wavefronts has a head to itself, so that nothing
+// has to be joined.  Else every split but a sequence's last holds whole rounds of four wavefronts (64 rows each, 32 above d_h =
+// 128), as few splits as leave about 1024 workgroups on the chip.
 constexpr int MX_MAX_SPLITS = 256;
 inline int mx_max_splits(long long groups, int T) {
   const long long want = groups < 1024 ? 1024 / groups : 1, rounds = (T + 127) / 128;
   const long long s = want < rounds ? want : rounds;
   return (int)(s < MX_MAX_SPLITS ? s : MX_MAX_SPLITS);
 }
-inline int mx_rows_per_split(long long groups, int T, int longest, int dh) {
-  const int unit = dh <= 128 ? 256 : 128, most = mx_max_splits(groups, T), even = (longest + most - 1) / most;
-  return even <= unit ? unit : (even + unit - 1) / unit * unit;
+struct MxSplit {
+  int n, rows;  // splits, rows of each
+  bool many;    // 16 (8) wavefronts to a workgroup, else 4
+};
+inline MxSplit mx_split(long long groups, int T, int longest, int dh) {
+  const int unit = dh <= 128 ? 256 : 128;
+  if (groups <= 256 && longest <= 2048) return {1, longest > 0 ? longest : 1, longest > unit};
+  const int most = mx_max_splits(groups, T), even = (longest + most - 1) / most;
+  const int rows = even <= unit ? unit : (even + unit - 1) / unit * unit;
+  return {longest > rows ? (longest + rows - 1) / rows : 1, rows, false};
 }
 
 }  // namespace cca
