@@ -379,20 +379,27 @@ __global__ __launch_bounds__(256) void mx_finish_kernel(AttnArgs a, int dh, long
     if (item < joins) {
       const int chunks = (dh + 63) / 64, c0 = (int)(item % chunks) * 64;
       const long long bh = item / chunks;
+      // splits wave, wave + 4, ...: the first 16 requested before anything is known of the sequence's length (a place that no split
+      // wrote is read, never used)
+      const float *src = a.part + bh * a.nsplit * dh + min(c0 + lane, dh - 1);
+      float v[16];
+#pragma unroll
+      for (int u = 0; u < 16; ++u) v[u] = src[(long long)min(wave + 4 * u, a.nsplit - 1) * dh];
       const int len = seq_len(a, (int)(bh / a.Hq)), n = max(1, min(a.nsplit, (len + a.per - 1) / a.per));
       const mx_f2 ml = joined(a.state + bh * a.nsplit, n, lane, st);  // every wavefront for itself
       const mx_f2 mine = wave == 0 ? st[0] : wave == 1 ? st[1] : wave == 2 ? st[2] : st[3];
       f[tid] = rescale(mine[0], mine[1], ml[0]);  // of split `tid`
       __syncthreads();
-      const int q = (n + 3) / 4, s0 = wave * q, s1 = min(n, s0 + q), ch = min(c0 + lane, dh - 1);
-      const float *src = a.part + bh * a.nsplit * dh + ch;
       float sum = 0.f;
-      for (int s = s0; s < s1; s += 16) {
-        float v[16];
 #pragma unroll
-        for (int u = 0; u < 16; ++u) v[u] = src[(long long)min(s + u, s1 - 1) * dh];
+      for (int u = 0; u < 16; ++u) sum = wave + 4 * u < n ? fmaf(v[u], f[wave + 4 * u], sum) : sum;
+#pragma unroll 1
+      for (int s = wave + 64; s < n; s += 96) {
+        float x[24];
 #pragma unroll
-        for (int u = 0; u < 16; ++u) sum = s + u < s1 ? fmaf(v[u], f[s + u], sum) : sum;
+        for (int u = 0; u < 24; ++u) x[u] = src[(long long)min(s + 4 * u, n - 1) * dh];
+#pragma unroll
+        for (int u = 0; u < 24; ++u) sum = s + 4 * u < n ? fmaf(x[u], f[min(s + 4 * u, 255)], sum) : sum;
       }
       acc[wave][lane] = sum;
       __syncthreads();

@@ -1,4 +1,6 @@
 // Projections with 4-bit weights, for the few rows of a decode step: y (M, N) = x (M, K) W, and the quantisation of W.
+#include <type_traits>
+
 #include "cca_mx.h"
 
 namespace cca {
@@ -15,78 +17,165 @@ struct ProjArgs {
   int M, K, N;
 };
 
-// x (8 numbers of a row from `at`) as TERMS parts in bf16
-template <typename T, int TERMS>
-__device__ __forceinline__ void load_x(const T *p, bool on, mx_bf8 (&f)[TERMS]) {
-  if constexpr (TERMS == 1) {
-    mx_u4 w = *reinterpret_cast<const mx_u4 *>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = on ? w[i] : 0u;
-    f[0] = __builtin_bit_cast(mx_bf8, w);
-  } else {
-    const mx_f4 a = *reinterpret_cast<const mx_f4 *>(p), b = *reinterpret_cast<const mx_f4 *>(p + 4);
-    float r[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = on ? r[i] : 0.f;
-#pragma unroll
-    for (int u = 0; u < TERMS; ++u) {
-      mx_u4 w;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t wi = mx_pack(r[2 * i], r[2 * i + 1]);
-        w[i] = wi;
-        r[2 * i] -= mx_lo(wi), r[2 * i + 1] -= mx_hi(wi);
-      }
-      f[u] = __builtin_bit_cast(mx_bf8, w);
-    }
-  }
-}
+// ---------------------------------------------------------------------------
+// Workgroup = 16 CT columns x up to ROWS rows; its eight wavefronts take 256 numbers of K in turn, 128 to a step (a line of a column's
+// codes) and their sums are added at the end, in order.  Lane (m, j) = (lane mod 16, lane / 16) takes 32 numbers of column m - 16 bytes, one
+// scale - which are the W operands of four products of 16 x 16 x 32.
+// x: each wavefront has its rows' 128 numbers loaded straight into LDS, two steps deep, and reads them as the products want them;
+// read by lanes from memory, every lane's 16 bytes lie in a line of their own, which took 38 us for 32 x 8192 x 8192.  16-byte chunk c of
+// row r lies at place c ^ r (fp32: pairs of chunks), so that 16 rows of one chunk fall into different banks.
+// fp32: x in three parts of bf16, three products.
+// ---------------------------------------------------------------------------
+template <typename T, int ROWS, int CT>
+struct ProjForm {
+  static constexpr int MT = ROWS < 16 ? 1 : ROWS / 16;
+  static constexpr int LINE = 128 * (int)sizeof(T), RPL = 1024 / LINE, XI = ROWS / RPL;  // bytes of a row's step; rows of a load; loads
+  static constexpr int SLAB = ROWS * LINE;                                              // bytes of a step of x
+  static constexpr size_t X = (size_t)WAVES * 2 * SLAB, SUMS = (size_t)WAVES * MT * 16 * (16 * CT + 1) * 4, LDS = X > SUMS ? X : SUMS;
+};
 
-// ---------------------------------------------------------------------------
-// Workgroup = 16 columns x 16 MT rows, its eight wavefronts share K.  Lane (m, j) takes 32 numbers of column m (16 bytes, one
-// scale) per 128 of K; four products of 16 x 16 x 32.
-// ---------------------------------------------------------------------------
-template <typename T, typename TO, int MT>
+template <typename T, typename TO, int ROWS, int CT>
 __global__ __launch_bounds__(WAVES * 64) void mx_project_kernel(ProjArgs a) {
-  constexpr int TERMS = sizeof(T) == 4 ? 3 : 1;
-  __shared__ float red[WAVES][MT][16][17];
+  typedef ProjForm<T, ROWS, CT> F;
+  constexpr int MT = F::MT, XI = F::XI, TERMS = sizeof(T) == 4 ? 3 : 1;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char proj_lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 15, j = lane >> 4;
-  const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * MT, col = min(n0 + m, a.N - 1), groups = a.K / 32;
-  const unsigned char *codes = a.codes + (long long)col * (a.K / 2), *scales = a.scales + (long long)col * groups;
-  const T *x = static_cast<const T *>(a.x);
-  mx_f4 acc[MT];
+  const int n0 = blockIdx.x * 16 * CT, groups = a.K / 32, steps = (groups + 3) / 4;
+  const int m0 = blockIdx.y * ROWS, rows = min(ROWS, a.M - m0);
+  const T *const x = static_cast<const T *>(a.x) + (long long)m0 * a.K;
+  const unsigned x_bytes = (unsigned)rows * (unsigned)a.K * (unsigned)sizeof(T);  // (32 rows of 65536 numbers at most)
+  unsigned char *const slab = proj_lds + wave * 2 * F::SLAB;
+  const unsigned char *codes[CT], *scales[CT];
 #pragma unroll
-  for (int t = 0; t < MT; ++t) acc[t] = mx_f4{0.f, 0.f, 0.f, 0.f};
-  const int steps = (groups + 3) / 4, per = (steps + WAVES - 1) / WAVES, s1 = min(steps, (wave + 1) * per);
-  for (int st = wave * per; st < s1; ++st) {
-    const int g = st * 4 + j, gc = min(g, groups - 1);
-    const bool on = g < groups;
-    const mx_u4 w = *reinterpret_cast<const mx_u4 *>(codes + gc * 16);
-    const uint32_t sc = on ? (uint32_t)scales[gc] << 23 : 0u;
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const mx_bf8 wf = mx_eight(w[s], sc);
-#pragma unroll
-      for (int t = 0; t < MT; ++t) {
-        mx_bf8 xf[TERMS];
-        load_x<T, TERMS>(x + (long long)min(m0 + 16 * t + m, a.M - 1) * a.K + gc * 32 + 8 * s, on, xf);
-#pragma unroll
-        for (int u = 0; u < TERMS; ++u) acc[t] = mx_mfma(wf, xf[u], acc[t]);
-      }
-    }
+  for (int c = 0; c < CT; ++c) {
+    const int col = min(n0 + 16 * c + m, a.N - 1);  // columns past the last repeat it; nobody stores them
+    codes[c] = a.codes + (long long)col * (a.K / 2);
+    scales[c] = a.scales + (long long)col * groups;
   }
+  mx_f4 acc[MT][CT];
 #pragma unroll
   for (int t = 0; t < MT; ++t)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) red[wave][t][m][4 * j + i] = acc[t][i];
+    for (int c = 0; c < CT; ++c) acc[t][c] = mx_f4{0.f, 0.f, 0.f, 0.f};
+
+  // this lane's place in a load of x: row (of RPL), chunk of it
+  constexpr int CPL = F::LINE / 16;
+  auto load_x = [&](int st, int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < XI; ++i) {
+      const int r = F::RPL * i + lane / CPL, c = (lane % CPL) ^ (sizeof(T) == 2 ? r & 15 : (r & 15) << 1);
+      const int k = st * 128 + c * (16 / (int)sizeof(T));
+      // numbers past K and rows past M are zero: they lie beyond the bytes that the load may touch
+      const unsigned off = k < a.K ? ((unsigned)r * (unsigned)a.K + (unsigned)k) * (unsigned)sizeof(T) : 0x40000000u;
+      load_to_lds(x, x_bytes, off, 0, slab + buf * F::SLAB + i * 1024);
+    }
+  };
+  auto load_w = [&](int pair, mx_u4 (&w)[2][CT], uint32_t (&sc)[2][CT]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int g = min((2 * pair + h) * 4 + j, groups - 1);
+        w[h][c] = *reinterpret_cast<const mx_u4 *>(codes[c] + g * 16);
+        sc[h][c] = scales[c][g];
+      }
+  };
+  auto multiply = [&](int st, int buf, const mx_u4 (&w)[CT], const uint32_t (&sc)[CT]) __attribute__((always_inline)) {
+    const bool on = st * 4 + j < groups;  // a group past K: scale 2^-127 times a zero of x
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      mx_bf8 wf[CT];
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        const uint32_t ws = w[c][s];
+        wf[c] = mx_eight(ws, on ? sc[c] << 23 : 0u);
+      }
+#pragma unroll
+      for (int t = 0; t < MT; ++t) {
+        const int r = ROWS < 16 ? m & (ROWS - 1) : m;  // (fewer than 16 rows: again, for columns of the product that nobody stores)
+        const unsigned char *const row = slab + buf * F::SLAB + (16 * t + r) * F::LINE;
+        if constexpr (sizeof(T) == 2) {
+          const mx_bf8 xf = __builtin_bit_cast(mx_bf8, *reinterpret_cast<const mx_u4 *>(row + (((4 * j + s) ^ r) * 16)));
+#pragma unroll
+          for (int c = 0; c < CT; ++c) acc[t][c] = mx_mfma(wf[c], xf, acc[t][c]);
+        } else {
+          const unsigned char *const at = row + (((8 * j + 2 * s) ^ (r << 1)) * 16);
+          const mx_f4 lo = *reinterpret_cast<const mx_f4 *>(at), hi = *reinterpret_cast<const mx_f4 *>(at + 16);
+          float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+#pragma unroll
+          for (int u = 0; u < TERMS; ++u) {
+            mx_u4 p;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t pi = mx_pack(v[2 * i], v[2 * i + 1]);
+              p[i] = pi;
+              v[2 * i] -= mx_lo(pi), v[2 * i + 1] -= mx_hi(pi);
+            }
+#pragma unroll
+            for (int c = 0; c < CT; ++c) acc[t][c] = mx_mfma(wf[c], __builtin_bit_cast(mx_bf8, p), acc[t][c]);
+          }
+        }
+      }
+    }
+  };
+
+  // A wavefront takes two steps at a time, so that it asks for whole lines of W: with every other 64 bytes to another wavefront, and
+  // columns a power of two apart, 1 x 8192 x 8192 took 10.5 us (K = 7936: 8.1).  Four steps under way instead of two gained nothing.
+  mx_u4 w[2][2][CT];
+  uint32_t sc[2][2][CT];
+  const int pairs = (steps + 1) / 2;
+  if (wave < pairs) {  // (each wavefront for itself: no barrier inside)
+    // Columns begin K / 2 bytes apart, often a multiple of the memory channels' turn: workgroups that walk K in step would all
+    // ask the same few channels.  Each begins at a pair of its own and goes round.
+    const int turns = (pairs - wave + WAVES - 1) / WAVES;
+    int p = wave + (int)(blockIdx.x % (unsigned)turns) * WAVES, left = turns;
+    load_w(p, w[0], sc[0]);
+    load_x(2 * p, 0);
+    auto half = [&](int st, auto h_, const mx_u4 (&wh)[CT], const uint32_t (&sh)[CT]) __attribute__((always_inline)) {
+      asm volatile("" ::: "memory");
+      multiply(st, decltype(h_)::value, wh, sh);
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_waitcnt(WAIT_LDS);  // the reads of this step are done before the next one loads over them
+    };
+    auto turn = [&](auto buf_) __attribute__((always_inline)) {
+      constexpr int buf = decltype(buf_)::value;
+      load_x(2 * p + 1, 1);
+      __builtin_amdgcn_s_waitcnt(wait_vm(XI));
+      half(2 * p, std::integral_constant<int, 0>{}, w[buf][0], sc[buf][0]);
+      const int next = p + WAVES < pairs ? p + WAVES : wave;
+      if (left > 1) {
+        load_w(next, w[buf ^ 1], sc[buf ^ 1]);
+        load_x(2 * next, 0);
+        __builtin_amdgcn_s_waitcnt(wait_vm(4 * CT + XI));
+      } else {
+        __builtin_amdgcn_s_waitcnt(wait_vm(0));
+      }
+      half(2 * p + 1, std::integral_constant<int, 1>{}, w[buf][1], sc[buf][1]);
+      p = next, --left;
+    };
+    while (true) {
+      turn(std::integral_constant<int, 0>{});
+      if (!left) break;
+      turn(std::integral_constant<int, 1>{});
+      if (!left) break;
+    }
+  }
   __syncthreads();
-  for (int i = tid; i < MT * 256; i += WAVES * 64) {
-    const int t = i / 256, r = i / 16 % 16, c = i % 16;
+  constexpr int RS = 16 * CT + 1;
+  float *const red = reinterpret_cast<float *>(proj_lds);  // [wave][row][column]
+#pragma unroll
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) red[((wave * MT + t) * 16 + m) * RS + 16 * c + 4 * j + i] = acc[t][c][i];
+  __syncthreads();
+  for (int i = tid; i < rows * 16 * CT; i += WAVES * 64) {
+    const int r = i / (16 * CT), c = i % (16 * CT);
     float sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) sum += red[w][t][r][c];
-    const int row = m0 + 16 * t + r;
-    if (row < a.M && n0 + c < a.N) store_f(static_cast<TO *>(a.y) + a.dest.at(row, a.N) + n0 + c, sum);
+    for (int wv = 0; wv < WAVES; ++wv) sum += red[(wv * MT * 16 + r) * RS + c];
+    if (n0 + c < a.N) store_f(static_cast<TO *>(a.y) + a.dest.at(m0 + r, a.N) + n0 + c, sum);
   }
 }
 
@@ -111,12 +200,24 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(const T *__restrict__ 
   scales[(long long)n * (K / 32) + g] = (unsigned char)s;
 }
 
+template <typename T, typename TO, int ROWS, int CT>
+hipError_t launch_form(const ProjArgs &a, hipStream_t s) {
+  constexpr size_t lds = ProjForm<T, ROWS, CT>::LDS;
+  if (hipError_t e = raise_lds_limit<mx_project_kernel<T, TO, ROWS, CT>>(lds); e != hipSuccess) return e;
+  mx_project_kernel<T, TO, ROWS, CT><<<dim3((a.N + 16 * CT - 1) / (16 * CT), (a.M + ROWS - 1) / ROWS), WAVES * 64, lds, s>>>(a);
+  return hipGetLastError();
+}
+template <typename T, typename TO, int ROWS>
+hipError_t launch_rows(const ProjArgs &a, hipStream_t s) {
+  return mx_project_wide(a.M, a.N, ROWS) ? launch_form<T, TO, ROWS, 2>(a, s) : launch_form<T, TO, ROWS, 1>(a, s);
+}
 template <typename T, typename TO>
 hipError_t launch(const ProjArgs &a, hipStream_t s) {
-  const unsigned cols = (a.N + 15) / 16;
-  if (a.M <= 16) mx_project_kernel<T, TO, 1><<<dim3(cols, 1), WAVES * 64, 0, s>>>(a);
-  else mx_project_kernel<T, TO, 2><<<dim3(cols, (a.M + 31) / 32), WAVES * 64, 0, s>>>(a);
-  return hipGetLastError();
+  const int rows = mx_project_rows(a.M, sizeof(T) == 4);
+  if (rows == 4) return launch_rows<T, TO, 4>(a, s);
+  if constexpr (sizeof(T) == 2)
+    if (rows == 32) return launch_rows<T, TO, 32>(a, s);
+  return launch_rows<T, TO, 16>(a, s);
 }
 
 }  // namespace

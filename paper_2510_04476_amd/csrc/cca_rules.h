@@ -483,4 +483,12 @@ inline MxSplit mx_split(long long groups, int T, int longest, int dh) {
   return {longest > rows ? (longest + rows - 1) / rows : 1, rows, false};
 }
 
+// ---- projections with 4-bit weights: rows of x to a workgroup, 16 or 32 columns ---------------------------------------------
+// x costs LDS, one workgroup of 16 or 32 rows to a CU, so columns are taken two tiles at a time where one tile to a workgroup would be more
+// than a round of the chip.  One tile -> two, us (M x K x N): 1 x 2048 x 1536 3.3, 4.2; 32 x 2048 x 4096 4.4, 5.4; 32 x 8192 x 4096 10.9, 14.0; beyond a
+// round 8 x 2048 x 5000 5.0, 4.6; 32 x 2048 x 5000 7.2, 5.6; 32 x 8192 x 8192 19.6, 15.1; fp32 8 x 8192 x 8192 25.2, 17.1; even for 1 x 8192 x 8192 10.8,
+// 11.1.  fp32 takes 16 rows at most: 32 would not fit the LDS.
+inline int mx_project_rows(int M, bool f32) { return M <= 4 ? 4 : M <= 16 || f32 ? 16 : 32; }
+inline bool mx_project_wide(int M, int N, int rows) { return (long long)((N + 15) / 16) * ((M + rows - 1) / rows) > 256; }
+
 }  // namespace cca
