@@ -31,19 +31,6 @@ struct AttnArgs {
 // 2^(m - M) for a part's maximum m and sum l; a part without rows has none
 __device__ __forceinline__ float rescale(float m, float l, float M) { return m == -INFINITY && l == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - M); }
 
-// weight_out[row ... row + 3] of a head = weight_in + sum, below len (the new rows of a step start from 0)
-__device__ __forceinline__ void add_weights(const AttnArgs &a, long long head, int row, int len, mx_f4 sum) {
-  const long long at = head * a.T + row;
-  if (row + 4 <= len - a.extra) {
-    if (a.weight_in) sum += *reinterpret_cast<const mx_f4 *>(a.weight_in + at);
-    *reinterpret_cast<mx_f4 *>(a.weight_out + at) = sum;
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (row + i < len) a.weight_out[at + i] = (a.weight_in && row + i < len - a.extra ? a.weight_in[at + i] : 0.f) + sum[i];
-}
-
 __device__ __forceinline__ int seq_len(const AttnArgs &a, int b) { return mx_clamp(a.len[b], 0, a.max_len) + a.extra; }
 
 // ---------------------------------------------------------------------------
@@ -69,12 +56,11 @@ struct Form {
   static constexpr int NG = N32 == 1 || N32 == 2 || N32 == 4 ? 1 : N32 == 8 ? 2 : (N32 + 2) / 4 + 1;  // groups that a lane's K channels touch
   static constexpr int COLS = TERMS == 1 ? 8 : 16;                // heads of a pass
   static constexpr int STRIDE = DH + 4;                           // floats of a head in the merge area: m, l, -, -, o
-  static constexpr int MANY = N32 <= 2 && TERMS < 3 ? 16 : 8;     // wavefronts of a workgroup that has its head to itself
   static constexpr int RESIDENT = N32 <= 2 ? 4 : N32 <= 4 && TERMS < 3 ? 3 : 2;  // wavefronts of a SIMD that the registers are held to
 };
 
 template <int N32, int TERMS, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, (WAVES == 4 ? Form<N32, TERMS>::RESIDENT : 1)) void mx_attn_kernel(AttnArgs a) {
+__global__ __launch_bounds__(WAVES * 64, (WAVES == 4 ? Form<N32, TERMS>::RESIDENT : 2)) void mx_attn_kernel(AttnArgs a) {
   typedef Form<N32, TERMS> F;
   constexpr int DH = F::DH, NT = F::NT, BLK = F::BLK, PB = F::PB, NP = F::NP, VT = F::VT, NG = F::NG;
   extern __shared__ __attribute__((aligned(16))) float mrg[];  // [WAVES][COLS][STRIDE]
@@ -349,11 +335,25 @@ __global__ __launch_bounds__(WAVES * 64, (WAVES == 4 ? Form<N32, TERMS>::RESIDEN
 }
 
 // ---------------------------------------------------------------------------
-// What follows the splits, in one launch.  The first workgroups join them: o = sum o_s 2^(m_s - M) / sum l_s 2^(m_s - M), 64 channels of a
-// query head each, a wavefront a quarter of the splits.  The others form the weights: weight_out[row] = weight_in[row] + sum over
+// What follows the splits, in one launch.  The first workgroups join them: o = sum o_s 2^(m_s - M) / sum l_s 2^(m_s - M), some channels
+// of a query head each.  The others form the weights: weight_out[row] = weight_in[row] + sum over
 // the R query heads of 2^(score - M) / L, four rows a thread.
 // ---------------------------------------------------------------------------
 constexpr int W_ROWS = 1024, W_HEADS = 16;
+__device__ __forceinline__ float wave_max(float x) {
+  x = fmaxf(x, mx_dpp<0xB1>(x));   // quad_perm [1,0,3,2]
+  x = fmaxf(x, mx_dpp<0x4E>(x));   // quad_perm [2,3,0,1]
+  x = fmaxf(x, mx_dpp<0x141>(x));  // row_half_mirror
+  x = fmaxf(x, mx_dpp<0x140>(x));  // row_mirror
+  return mx_xor32_max(mx_xor16_max(x));
+}
+__device__ __forceinline__ float wave_sum(float x) {
+  x += mx_dpp<0xB1>(x);
+  x += mx_dpp<0x4E>(x);
+  x += mx_dpp<0x141>(x);
+  x += mx_dpp<0x140>(x);
+  return mx_xor32_add(mx_xor16_add(x));
+}
 // m and l of a head over its n <= 256 splits, by a wavefront
 __device__ __forceinline__ mx_f2 joined(const mx_f2 *state, int n, int lane, mx_f2 (&st)[4]) {
   float M = -INFINITY;
@@ -363,28 +363,28 @@ __device__ __forceinline__ mx_f2 joined(const mx_f2 *state, int n, int lane, mx_
     if (64 * i + lane >= n) st[i] = mx_f2{-INFINITY, 0.f};
     M = fmaxf(M, st[i][0]);
   }
-  for (int off = 32; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
+  M = wave_max(M);
   float L = 0.f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) L += st[i][1] * rescale(st[i][0], st[i][1], M);
-  for (int off = 32; off > 0; off >>= 1) L += __shfl_xor(L, off);
-  return mx_f2{M, L};
+  return mx_f2{M, wave_sum(L)};
 }
-template <typename T>
+// CH: channels of a workgroup that joins; 256 / CH parts of it share the splits, 16 each, so that all are requested at once.
+template <typename T, int CH>
 __global__ __launch_bounds__(256) void mx_finish_kernel(AttnArgs a, int dh, long long joins, int tiles) {
-  __shared__ float f[256], acc[4][64], top[W_HEADS], inv[W_HEADS];
+  constexpr int PARTS = 256 / CH;
+  __shared__ float f[256], acc[PARTS][CH], top[W_HEADS], inv[W_HEADS];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   for (long long item = blockIdx.x; item < joins + (long long)a.B * a.Hk * tiles; item += gridDim.x, __syncthreads()) {
     mx_f2 st[4];
     if (item < joins) {
-      const int chunks = (dh + 63) / 64, c0 = (int)(item % chunks) * 64;
+      const int chunks = (dh + CH - 1) / CH, part = tid / CH, ch = (int)(item % chunks) * CH + tid % CH;
       const long long bh = item / chunks;
-      // splits wave, wave + 4, ...: the first 16 requested before anything is known of the sequence's length (a place that no split
-      // wrote is read, never used)
-      const float *src = a.part + bh * a.nsplit * dh + min(c0 + lane, dh - 1);
+      // requested before anything is known of the sequence's length (a place that no split wrote is read, never used)
+      const float *src = a.part + bh * a.nsplit * dh + min(ch, dh - 1);
       float v[16];
 #pragma unroll
-      for (int u = 0; u < 16; ++u) v[u] = src[(long long)min(wave + 4 * u, a.nsplit - 1) * dh];
+      for (int u = 0; u < 16; ++u) v[u] = src[(long long)min(part + PARTS * u, a.nsplit - 1) * dh];
       const int len = seq_len(a, (int)(bh / a.Hq)), n = max(1, min(a.nsplit, (len + a.per - 1) / a.per));
       const mx_f2 ml = joined(a.state + bh * a.nsplit, n, lane, st);  // every wavefront for itself
       const mx_f2 mine = wave == 0 ? st[0] : wave == 1 ? st[1] : wave == 2 ? st[2] : st[3];
@@ -392,54 +392,61 @@ __global__ __launch_bounds__(256) void mx_finish_kernel(AttnArgs a, int dh, long
       __syncthreads();
       float sum = 0.f;
 #pragma unroll
-      for (int u = 0; u < 16; ++u) sum = wave + 4 * u < n ? fmaf(v[u], f[wave + 4 * u], sum) : sum;
-#pragma unroll 1
-      for (int s = wave + 64; s < n; s += 96) {
-        float x[24];
-#pragma unroll
-        for (int u = 0; u < 24; ++u) x[u] = src[(long long)min(s + 4 * u, n - 1) * dh];
-#pragma unroll
-        for (int u = 0; u < 24; ++u) sum = s + 4 * u < n ? fmaf(x[u], f[min(s + 4 * u, 255)], sum) : sum;
-      }
-      acc[wave][lane] = sum;
+      for (int u = 0; u < 16; ++u) sum = part + PARTS * u < n ? fmaf(v[u], f[part + PARTS * u], sum) : sum;
+      acc[part][tid % CH] = sum;
       __syncthreads();
-      if (wave == 0) {
-        const float all = (acc[0][lane] + acc[1][lane]) + (acc[2][lane] + acc[3][lane]);
-        if (c0 + lane < dh) store_f(static_cast<T *>(a.o) + bh * dh + c0 + lane, ml[1] == 0.f ? 0.f : all / ml[1]);
-        if (c0 == 0 && lane == 0 && a.lse) a.lse[bh] = (ml[0] + log2f(ml[1])) * 0.69314718055994530942f;
+      if (part == 0) {
+        float all = 0.f;
+#pragma unroll
+        for (int x = 0; x < PARTS; ++x) all += acc[x][tid % CH];
+        if (ch < dh) store_f(static_cast<T *>(a.o) + bh * dh + ch, ml[1] == 0.f ? 0.f : all / ml[1]);
+        if (ch == 0 && a.lse) a.lse[bh] = (ml[0] + log2f(ml[1])) * 0.69314718055994530942f;
       }
       continue;
     }
     const long long head = (item - joins) / tiles;
-    const int b = (int)(head / a.Hk), g = (int)(head % a.Hk), len = seq_len(a, b), row0 = (int)((item - joins) % tiles) * W_ROWS, row = row0 + 4 * tid;
+    const int b = (int)(head / a.Hk), g = (int)(head % a.Hk), len = seq_len(a, b), row0 = (int)((item - joins) % tiles) * W_ROWS;
     if (row0 >= len) continue;
-    const int n = min(a.nsplit, (len + a.per - 1) / a.per);
-    mx_f4 sum = {0.f, 0.f, 0.f, 0.f};
+    const int n = min(a.nsplit, (len + a.per - 1) / a.per), old = len - a.extra;  // the new rows of a step start from 0
+    const int row = row0 + 4 * tid, at = min(row, a.T - 4);  // rows past the capacity are read at its end, never stored
+    mx_f4 sum = {0.f, 0.f, 0.f, 0.f}, before = sum;
+    if (a.weight_in) before = *reinterpret_cast<const mx_f4 *>(a.weight_in + head * a.T + at);
     for (int r0 = 0; r0 < a.R; r0 += W_HEADS) {
       const int nr = min(W_HEADS, a.R - r0);
       const long long h0 = (long long)b * a.Hq + g * a.R + r0;
+      const float *const sc = a.scores + h0 * a.T + at;
+      mx_f4 s[4];
+      auto request = [&](int r) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) s[u] = *reinterpret_cast<const mx_f4 *>(sc + (long long)min(r + u, nr - 1) * a.T);
+      };
+      request(0);  // with the states: one latency for both
       if (r0) __syncthreads();
       for (int r = wave; r < nr; r += 4) {
         const mx_f2 ml = joined(a.state + (h0 + r) * a.nsplit, n, lane, st);
         if (lane == 0) top[r] = ml[0] == -INFINITY ? 0.f : ml[0], inv[r] = ml[1] == 0.f ? 0.f : 1.f / ml[1];
       }
       __syncthreads();
-      if (row < len) {
-        const float *sc = a.scores + h0 * a.T + row;
-        for (int r = 0; r < nr; r += 4) {
-          mx_f4 s[4];
+      for (int r = 0; r < nr; r += 4) {
+        if (r) request(r);
 #pragma unroll
-          for (int u = 0; u < 4; ++u) s[u] = *reinterpret_cast<const mx_f4 *>(sc + (long long)min(r + u, nr - 1) * a.T);
+        for (int u = 0; u < 4; ++u)
+          if (r + u < nr) {
 #pragma unroll
-          for (int u = 0; u < 4; ++u)
-            if (r + u < nr) {
-#pragma unroll
-              for (int i = 0; i < 4; ++i) sum[i] = fmaf(__builtin_amdgcn_exp2f(s[u][i] - top[r + u]), inv[r + u], sum[i]);
-            }
-        }
+            for (int i = 0; i < 4; ++i) sum[i] = fmaf(__builtin_amdgcn_exp2f(s[u][i] - top[r + u]), inv[r + u], sum[i]);
+          }
       }
     }
-    add_weights(a, head, row, len, sum);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] += row + i < old ? before[i] : 0.f;
+    float *const to = a.weight_out + head * a.T + row;
+    if (row + 4 <= len) {
+      *reinterpret_cast<mx_f4 *>(to) = sum;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (row + i < len) to[i] = sum[i];
+    }
   }
 }
 
@@ -455,7 +462,7 @@ hipError_t launch_waves(const AttnArgs &a, hipStream_t s) {
 }
 template <int N32, int TERMS>
 hipError_t launch(const AttnArgs &a, bool many, hipStream_t s) {
-  return many ? launch_waves<N32, TERMS, Form<N32, TERMS>::MANY>(a, s) : launch_waves<N32, TERMS, 4>(a, s);
+  return many ? launch_waves<N32, TERMS, 8>(a, s) : launch_waves<N32, TERMS, 4>(a, s);
 }
 template <int TERMS>
 hipError_t launch_width(int n32, const AttnArgs &a, bool many, hipStream_t s) {
@@ -478,7 +485,7 @@ Layout layout(const Dims &d) {
   Layout L;
   size_t off = 0;
   auto take = [&](size_t n) { const size_t at = off; off += align256(n); return at; };
-  const size_t splits = (size_t)d.B * d.Hq * mx_max_splits((long long)d.B * d.Hk, d.T);
+  const size_t splits = (size_t)d.B * d.Hq * mx_max_splits((long long)d.B * d.Hk, d.T, d.dh);
   L.state = take(splits * sizeof(mx_f2));
   L.part = take(splits * d.dh * sizeof(float));
   L.scores = take((size_t)d.B * d.Hq * d.T * sizeof(float));
@@ -496,7 +503,7 @@ hipError_t mx_attention(const Dims &d, const cca_mx_cache &c, const void *q, boo
   unsigned char *ws = static_cast<unsigned char *>(workspace);
   const int longest = max_len + extra;
   const long long groups = (long long)d.B * d.Hk;
-  const MxSplit split = mx_split(groups, d.T, longest, d.dh);
+  const MxSplit split = mx_split(groups, d.T, longest, d.dh, weight_out != nullptr);
   const bool finish = split.n > 1 || weight_out;
   auto p = [](const void *x) { return static_cast<const unsigned char *>(x); };
   AttnArgs a{d.B, d.T, d.Hq, d.Hk, d.R, max_len, extra, split.n, split.rows, 0, d.scale * 1.44269504088896340736f, len, q, q_f32 || !d.bf16,
@@ -512,10 +519,13 @@ hipError_t mx_attention(const Dims &d, const cca_mx_cache &c, const void *q, boo
   }
   if (!finish) return hipSuccess;
   const int tiles = weight_out ? (longest + W_ROWS - 1) / W_ROWS : 0;
-  const long long joins = (long long)d.B * d.Hq * ((d.dh + 63) / 64), items = joins + groups * tiles;
+  const int ch = split.n <= 64 ? 64 : 16;
+  const long long joins = (long long)d.B * d.Hq * ((d.dh + ch - 1) / ch), items = joins + groups * tiles;
   const unsigned grid = (unsigned)(items < (1 << 20) ? items : 1 << 20);
-  if (d.bf16) mx_finish_kernel<bf16_t><<<grid, 256, 0, s>>>(a, d.dh, joins, tiles);
-  else mx_finish_kernel<float><<<grid, 256, 0, s>>>(a, d.dh, joins, tiles);
+  if (d.bf16 && ch == 64) mx_finish_kernel<bf16_t, 64><<<grid, 256, 0, s>>>(a, d.dh, joins, tiles);
+  else if (d.bf16) mx_finish_kernel<bf16_t, 16><<<grid, 256, 0, s>>>(a, d.dh, joins, tiles);
+  else if (ch == 64) mx_finish_kernel<float, 64><<<grid, 256, 0, s>>>(a, d.dh, joins, tiles);
+  else mx_finish_kernel<float, 16><<<grid, 256, 0, s>>>(a, d.dh, joins, tiles);
   return hipGetLastError();
 }
 

@@ -107,9 +107,10 @@ def test_attention(i):
     o, lse = P.cca_decode_attention_mx(cfg, cache, q, i32(lens), T, want_lse=True, weight_in=cache.weight, weight_out=w)
     torch.cuda.synchronize()
     check_attention(cfg, vals, q, lens, o, lse, w, cache.weight, before)
-    # without weights, with the least bound on the lengths, and with fresh weights: the same
+    # without weights (the splits of the rows may be others then), with the least bound on the lengths, and with fresh weights
     o2, lse2 = P.cca_decode_attention_mx(cfg, cache, q, i32(lens), T, want_lse=True)
-    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+    torch.cuda.synchronize()
+    check_attention(cfg, vals, q, lens, o2, lse2)
     o3, lse3 = P.cca_decode_attention_mx(cfg, cache, q, i32(lens), max(lens), want_lse=True, weight_out=w.copy_(before))
     torch.cuda.synchronize()
     check_attention(cfg, vals, q, lens, o3, lse3, w, None, before)
