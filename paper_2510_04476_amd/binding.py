@@ -526,6 +526,14 @@ def _mx_opt(name, t, shape, dtype, index):
     return None if t is None else _mx_ptr(name, t, shape, dtype, index)
 
 
+def _mx_out(name, t, shape, dtype, index, like):
+    """An output and its address: `t`, or a new tensor on the device of `like`."""
+    if t is not None:
+        return t, _mx_ptr(name, t, shape, dtype, index)
+    t = like.new_empty(shape, dtype=dtype)
+    return t, t.data_ptr()
+
+
 def _mx_call(where, index, *args):
     """A call on the tensors' device and on that device's current stream."""
     if index < 0:
@@ -621,9 +629,9 @@ def cca_project_mx(x: torch.Tensor, w: CCAMXWeight, out: torch.Tensor | None = N
     if (dt is not torch.bfloat16 and dt is not torch.float32) or not shape or shape[-1] != w.K:
         raise ValueError(f"cca_project_mx: x {dt} {tuple(shape)}, weight of K = {w.K}")
     y_shape = (*shape[:-1], w.N)
-    out = x.new_empty(y_shape) if out is None else out
-    _mx_call("cca_project_mx", index, _mx_ptr("x", x, shape, dt, index), w._ref, _mx_ptr("out", out, y_shape, dt, index), x.numel() // w.K,
-             w.K, w.N, CCA_BF16 if dt is torch.bfloat16 else CCA_F32)
+    x_ptr = _mx_ptr("x", x, shape, dt, index)
+    out, out_ptr = _mx_out("out", out, y_shape, dt, index, x)
+    _mx_call("cca_project_mx", index, x_ptr, w._ref, out_ptr, x.numel() // w.K, w.K, w.N, CCA_BF16 if dt is torch.bfloat16 else CCA_F32)
     return out
 
 
@@ -642,9 +650,9 @@ def cca_cache_rows_mx(cfg: CCAConfig, cache: CCAMXCache, n: int, first=None, cou
     """(k, v), (B, n, H_k, d_h): rows first[b] ... (None: 0 ...) of every sequence, zero from the count[b]-th on (None: none)."""
     index, dt, per_seq = cache._index, cfg.torch_dtype, (cfg.B,)
     shape = (cfg.B, n, cfg.n_kv_heads, cfg.head_dim)
-    k = torch.empty(shape, dtype=dt, device=cache._device) if k is None else k
-    v = torch.empty(shape, dtype=dt, device=cache._device) if v is None else v
-    _mx_call("cca_cache_rows_mx", index, cfg.ref(), cache._for(cfg), _mx_ptr("k", k, shape, dt, index), _mx_ptr("v", v, shape, dt, index), n,
+    k, k_ptr = _mx_out("k", k, shape, dt, index, cache.k_codes)
+    v, v_ptr = _mx_out("v", v, shape, dt, index, cache.k_codes)
+    _mx_call("cca_cache_rows_mx", index, cfg.ref(), cache._for(cfg), k_ptr, v_ptr, n,
              _mx_opt("first", first, per_seq, torch.int32, index), _mx_opt("count", count, per_seq, torch.int32, index))
     return k, v
 
@@ -654,16 +662,15 @@ def cca_decode_attention_mx(cfg: CCAConfig, cache: CCAMXCache, q, lens, max_len:
     """o (B, H_q*d_h): attention of one query per sequence, q (B, H_q, d_h), over the first lens[b] <= max_len rows (int32 device
     tensor).  With weight_out (B, H_k, T) each of those rows' weight_in (None: 0) plus the attention it got goes there."""
     index, dt, B, Hq, dh = cache._index, cfg.torch_dtype, cfg.B, cfg.n_q_heads, cfg.head_dim
-    if o is None:
-        o = torch.empty((B, Hq * dh), dtype=dt, device=cache._device)
-    if lse is None and want_lse:
-        lse = torch.empty((B, Hq), dtype=torch.float32, device=cache._device)
+    o, o_ptr = _mx_out("o", o, (B, Hq * dh), dt, index, cache.k_codes)
+    lse_ptr = None
+    if lse is not None or want_lse:
+        lse, lse_ptr = _mx_out("lse", lse, (B, Hq), torch.float32, index, cache.k_codes)
     if workspace is None:
         workspace = new_mx_workspace(cfg, cache._device)
     w = (B, cfg.n_kv_heads, cfg.T)
     _mx_call("cca_decode_attention_mx", index, cfg.ref(), cache._for(cfg), _mx_ptr("q", q, (B, Hq, dh), dt, index),
-             _mx_ptr("lens", lens, (B,), torch.int32, index), max_len, _mx_ptr("o", o, (B, Hq * dh), dt, index),
-             _mx_opt("lse", lse, (B, Hq), torch.float32, index), _mx_opt("weight_in", weight_in, w, torch.float32, index),
+             _mx_ptr("lens", lens, (B,), torch.int32, index), max_len, o_ptr, lse_ptr, _mx_opt("weight_in", weight_in, w, torch.float32, index),
              _mx_opt("weight_out", weight_out, w, torch.float32, index),
              _mx_ptr("workspace", workspace, workspace.shape, torch.uint8, index), workspace.numel())
     return (o, lse) if want_lse else o
@@ -711,14 +718,14 @@ def cca_decode_step_mx(cfg: CCAConfig, w: CCAWeights, w_down: CCAMXWeight, w_out
     int32 device tensors, not advanced).  Of `w` the convolution filters and the temperatures are read."""
     index, dt, B, E = state.cache._index, cfg.torch_dtype, cfg.B, cfg.d_model
     x_shape, per_seq, ws = (B, E), (B,), state.workspace
-    out = torch.empty(x_shape, dtype=dt, device=state.cache._device) if out is None else out
+    out, out_ptr = _mx_out("out", out, x_shape, dt, index, state.cache.k_codes)
     for name, q, k, n in (("w_down", w_down, E, cfg.n_lat), ("w_out", w_out, cfg.e_q, E)):
         if q.K != k or q.N != n or q._index != index:
             raise ValueError(f"{name}: of (K, N) = {(q.K, q.N)} on {q.codes.device}, expected {(k, n)} on {state.cache._device}")
     cw, ring = w.c(), (B, cfg.ring_rows(), cfg.n_lat)
     _mx_call("cca_decode_step_mx", index, cfg.ref(), C.byref(cw), w_down._ref, w_out._ref, _mx_ptr("x_new", x_new, x_shape, dt, index),
              state.cache._for(cfg), _mx_ptr("lat_ring", state.lat_ring, ring, dt, index), _mx_ptr("pos", pos, per_seq, torch.int32, index),
-             _mx_ptr("lens", lens, per_seq, torch.int32, index), max_len, _mx_ptr("out", out, x_shape, dt, index),
+             _mx_ptr("lens", lens, per_seq, torch.int32, index), max_len, out_ptr,
              _mx_ptr("workspace", ws, ws.shape, torch.uint8, index), ws.numel())
     return out
 

@@ -1,4 +1,6 @@
 // The latent cache in 4 bits: rows stored, read back, and evicted by accumulated attention weight (include/cca.h).
+#include <type_traits>
+
 #include "cca_mx.h"
 
 namespace cca {
@@ -14,7 +16,7 @@ constexpr int TOK = 64;  // tokens of a workgroup
 // side by side: they go through LDS so that a wavefront stores them along the tokens.
 // ---------------------------------------------------------------------------
 struct StoreArgs {
-  int n, Hk, dh, T, max_row;
+  int n, Hk, T, max_row;
   long long tiles;  // B * 2 H_k * ceil(n / 64): K's heads of a sequence, then V's
 
   const int *rows, *counts, *pos;
@@ -45,70 +47,98 @@ __device__ __forceinline__ uint32_t group_scale(const float (&x)[8]) {
   return mx_scale_of(a);
 }
 
-template <typename T>
+// Where a workgroup's 64 tokens lie
+struct Tile {
+  int t0, b, row0, live;  // first token; sequence; its first row and how many of its n tokens are rows
+  long long head;
+  bool is_v;
+};
+__device__ __forceinline__ Tile tile_of(const StoreArgs &a, long long tile) {
+  const int per = (a.n + TOK - 1) / TOK;
+  Tile t;
+  const int hv = (int)(tile / per % (2 * a.Hk));
+  t.t0 = (int)(tile % per) * TOK;
+  t.b = (int)(tile / per / (2 * a.Hk));
+  t.is_v = hv >= a.Hk;
+  t.head = (long long)t.b * a.Hk + hv % a.Hk;
+  t.row0 = a.rows ? mx_clamp(a.rows[t.b], 0, a.max_row) : 0;
+  t.live = min(mx_clamp(a.counts ? a.counts[t.b] : a.n, 0, a.n), a.T - t.row0);
+  return t;
+}
+
+// (16-byte pieces of the 64 tokens: N32 = d_h / 32 to a thread, all requested before the first is used)
+template <typename T, int N32>
 __global__ __launch_bounds__(256) void mx_store_kernel(StoreArgs a, const T *__restrict__ k, const T *__restrict__ v,
                                                       unsigned char *__restrict__ k_codes, unsigned char *__restrict__ k_scales,
                                                       unsigned char *__restrict__ v_codes, unsigned char *__restrict__ v_scales) {
-  __shared__ unsigned char sc[8][TOK];  // (d_h / 32 <= 8 groups)
-  const int tid = threadIdx.x, per = (a.n + TOK - 1) / TOK;
+  constexpr int DH = 32 * N32, LPR = DH / 8;
+  __shared__ unsigned char sc[N32][TOK];
+  const int tid = threadIdx.x;
   for (long long tile = blockIdx.x; tile < a.tiles; tile += gridDim.x, __syncthreads()) {
-    const int t0 = (int)(tile % per) * TOK, hv = (int)(tile / per % (2 * a.Hk)), h = hv % a.Hk, b = (int)(tile / per / (2 * a.Hk));
-    const bool is_v = hv >= a.Hk;
-    const int row0 = mx_clamp(a.rows[b], 0, a.max_row), live = min(mx_clamp(a.counts ? a.counts[b] : a.n, 0, a.n), a.T - row0);
-    const int nt = min(TOK, live - t0);
+    const Tile t = tile_of(a, tile);
+    const int nt = min(TOK, t.live - t.t0), h = (int)(t.head % a.Hk);
     if (nt <= 0) continue;
-    const T *src = (is_v ? v : k) + ((long long)b * a.n * a.Hk + h) * a.dh;
-    const long long head = (long long)b * a.Hk + h;
-    unsigned char *codes = (is_v ? v_codes : k_codes) + (head * a.T + row0) * (a.dh / 2);
-    const int lpr = a.dh / 8;  // lanes of a row
-    for (int i = tid; i < nt * lpr; i += 256) {  // (a multiple of 4 lanes: a group's lanes are together)
-      const int t = i / lpr, c = i % lpr;
-      float x[8];
-      load8(src + (long long)(t0 + t) * a.Hk * a.dh + c * 8, x);
-      const uint32_t s = group_scale(x);
-      *reinterpret_cast<uint32_t *>(codes + (long long)(t0 + t) * (a.dh / 2) + c * 4) = mx_codes(x, s);
-      if ((c & 3) == 0) sc[c >> 2][t] = (unsigned char)s;
+    const T *src = (t.is_v ? v : k) + (((long long)t.b * a.n + t.t0) * a.Hk + h) * DH;
+    unsigned char *codes = (t.is_v ? v_codes : k_codes) + (t.head * a.T + t.row0 + t.t0) * (DH / 2);
+    float x[N32][8];
+#pragma unroll
+    for (int u = 0; u < N32; ++u) {
+      const int i = u * 256 + tid, tok = min(i / LPR, nt - 1), c = i % LPR;  // tokens past the last repeat it; nobody stores them
+      load8(src + (long long)tok * a.Hk * DH + c * 8, x[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < N32; ++u) {
+      const int i = u * 256 + tid, tok = i / LPR, c = i % LPR;
+      const uint32_t s = group_scale(x[u]);  // (four lanes of one token)
+      if (tok >= nt) continue;
+      *reinterpret_cast<uint32_t *>(codes + tok * (DH / 2) + c * 4) = mx_codes(x[u], s);
+      if ((c & 3) == 0) sc[c >> 2][tok] = (unsigned char)s;
     }
     __syncthreads();
-    unsigned char *scales = (is_v ? v_scales : k_scales) + head * (a.dh / 32) * a.T + row0 + t0;
-    for (int i = tid; i < a.dh / 32 * TOK; i += 256)
+    unsigned char *scales = (t.is_v ? v_scales : k_scales) + t.head * N32 * a.T + t.row0 + t.t0;
+#pragma unroll
+    for (int i = tid; i < N32 * TOK; i += 256)
       if (i % TOK < nt) scales[(long long)(i / TOK) * a.T + i % TOK] = sc[i / TOK][i % TOK];
-    if (!is_v && tid < nt) {
-      const long long at = head * a.T + row0 + t0 + tid;
-      if (a.row_pos) a.row_pos[at] = (a.pos ? a.pos[b] : row0) + t0 + tid;
+    if (!t.is_v && tid < nt) {
+      const long long at = t.head * a.T + t.row0 + t.t0 + tid;
+      if (a.row_pos) a.row_pos[at] = (a.pos ? a.pos[t.b] : t.row0) + t.t0 + tid;
       if (a.weight) a.weight[at] = 0.f;
     }
   }
 }
 
 // Read back: the same workgroups the other way round
-template <typename T>
+template <typename T, int N32>
 __global__ __launch_bounds__(256) void mx_rows_kernel(StoreArgs a, T *__restrict__ k, T *__restrict__ v,
                                                      const unsigned char *__restrict__ k_codes, const unsigned char *__restrict__ k_scales,
                                                      const unsigned char *__restrict__ v_codes, const unsigned char *__restrict__ v_scales) {
-  __shared__ unsigned char sc[8][TOK];
-  const int tid = threadIdx.x, per = (a.n + TOK - 1) / TOK;
+  constexpr int DH = 32 * N32, LPR = DH / 8;
+  __shared__ unsigned char sc[N32][TOK];
+  const int tid = threadIdx.x;
   for (long long tile = blockIdx.x; tile < a.tiles; tile += gridDim.x, __syncthreads()) {
-    const int t0 = (int)(tile % per) * TOK, hv = (int)(tile / per % (2 * a.Hk)), h = hv % a.Hk, b = (int)(tile / per / (2 * a.Hk));
-    const bool is_v = hv >= a.Hk;
-    const int row0 = a.rows ? mx_clamp(a.rows[b], 0, a.max_row) : 0, live = min(mx_clamp(a.counts ? a.counts[b] : a.n, 0, a.n), a.T - row0);
-    const int nt = min(TOK, a.n - t0), nl = live - t0;  // tokens of this workgroup; those of them that are rows
-    const long long head = (long long)b * a.Hk + h;
-    const unsigned char *codes = (is_v ? v_codes : k_codes) + (head * a.T + row0) * (a.dh / 2);
-    const unsigned char *scales = (is_v ? v_scales : k_scales) + head * (a.dh / 32) * a.T + row0 + t0;
-    for (int i = tid; i < a.dh / 32 * TOK; i += 256)
-      if (i % TOK < nl) sc[i / TOK][i % TOK] = scales[(long long)(i / TOK) * a.T + i % TOK];
-    __syncthreads();
-    T *dst = (is_v ? v : k) + ((long long)b * a.n * a.Hk + h) * a.dh;
-    const int lpr = a.dh / 8;
-    for (int i = tid; i < nt * lpr; i += 256) {
-      const int t = i / lpr, c = i % lpr;
-      mx_u4 w = {0, 0, 0, 0};
-      if (t < nl) {
-        const uint32_t code = *reinterpret_cast<const uint32_t *>(codes + (long long)(t0 + t) * (a.dh / 2) + c * 4);
-        w = __builtin_bit_cast(mx_u4, mx_eight(code, (uint32_t)sc[c >> 2][t] << 23));
+    const Tile t = tile_of(a, tile);
+    const int nt = min(TOK, a.n - t.t0), nl = t.live - t.t0, h = (int)(t.head % a.Hk);  // tokens of this workgroup; those of them that are rows
+    uint32_t code[N32];
+    if (nl > 0) {
+      const unsigned char *codes = (t.is_v ? v_codes : k_codes) + (t.head * a.T + t.row0 + t.t0) * (DH / 2);
+      const unsigned char *scales = (t.is_v ? v_scales : k_scales) + t.head * N32 * a.T + t.row0 + t.t0;
+#pragma unroll
+      for (int u = 0; u < N32; ++u) {
+        const int i = u * 256 + tid;
+        code[u] = *reinterpret_cast<const uint32_t *>(codes + min(i / LPR, nl - 1) * (DH / 2) + i % LPR * 4);
       }
-      T *to = dst + (long long)(t0 + t) * a.Hk * a.dh + c * 8;
+#pragma unroll
+      for (int i = tid; i < N32 * TOK; i += 256) sc[i / TOK][i % TOK] = scales[(long long)(i / TOK) * a.T + min(i % TOK, nl - 1)];
+    }
+    __syncthreads();
+    T *dst = (t.is_v ? v : k) + (((long long)t.b * a.n + t.t0) * a.Hk + h) * DH;
+#pragma unroll
+    for (int u = 0; u < N32; ++u) {
+      const int i = u * 256 + tid, tok = i / LPR, c = i % LPR;
+      if (tok >= nt) continue;
+      mx_u4 w = {0, 0, 0, 0};
+      if (tok < nl) w = __builtin_bit_cast(mx_u4, mx_eight(code[u], (uint32_t)sc[c >> 2][tok] << 23));
+      T *to = dst + (long long)tok * a.Hk * DH + c * 8;
       if constexpr (sizeof(T) == 2) {
         *reinterpret_cast<mx_u4 *>(to) = w;
       } else {
@@ -385,23 +415,43 @@ long long store_tiles(const Dims &d, int n) { return (long long)d.B * 2 * d.Hk *
 
 }  // namespace
 
-hipError_t mx_store(const Dims &d, const cca_mx_cache &c, const void *k, const void *v, int n, const int *rows, int max_row,
-                    const int *counts, const int *pos, hipStream_t s) {
-  const StoreArgs a{n, d.Hk, d.dh, d.T, max_row, store_tiles(d, n), rows, counts, pos, reinterpret_cast<int *>(c.pos), c.weight};
-  const unsigned grid = (unsigned)(a.tiles < MAX_GRID ? a.tiles : MAX_GRID);
-  auto p = [](void *x) { return static_cast<unsigned char *>(x); };
-  if (d.bf16) mx_store_kernel<bf16_t><<<grid, 256, 0, s>>>(a, (const bf16_t *)k, (const bf16_t *)v, p(c.k_codes), p(c.k_scales), p(c.v_codes), p(c.v_scales));
-  else mx_store_kernel<float><<<grid, 256, 0, s>>>(a, (const float *)k, (const float *)v, p(c.k_codes), p(c.k_scales), p(c.v_codes), p(c.v_scales));
+// f(integral constant of d_h / 32)
+template <typename F>
+static hipError_t by_width(int dh, F f) {
+  switch (dh / 32) {
+    case 1: f(std::integral_constant<int, 1>{}); break;
+    case 2: f(std::integral_constant<int, 2>{}); break;
+    case 3: f(std::integral_constant<int, 3>{}); break;
+    case 4: f(std::integral_constant<int, 4>{}); break;
+    case 5: f(std::integral_constant<int, 5>{}); break;
+    case 6: f(std::integral_constant<int, 6>{}); break;
+    case 7: f(std::integral_constant<int, 7>{}); break;
+    default: f(std::integral_constant<int, 8>{}); break;
+  }
   return hipGetLastError();
 }
 
+hipError_t mx_store(const Dims &d, const cca_mx_cache &c, const void *k, const void *v, int n, const int *rows, int max_row,
+                    const int *counts, const int *pos, hipStream_t s) {
+  const StoreArgs a{n, d.Hk, d.T, max_row, store_tiles(d, n), rows, counts, pos, reinterpret_cast<int *>(c.pos), c.weight};
+  const unsigned grid = (unsigned)(a.tiles < MAX_GRID ? a.tiles : MAX_GRID);
+  auto p = [](void *x) { return static_cast<unsigned char *>(x); };
+  return by_width(d.dh, [&](auto w) {
+    constexpr int N32 = decltype(w)::value;
+    if (d.bf16) mx_store_kernel<bf16_t, N32><<<grid, 256, 0, s>>>(a, (const bf16_t *)k, (const bf16_t *)v, p(c.k_codes), p(c.k_scales), p(c.v_codes), p(c.v_scales));
+    else mx_store_kernel<float, N32><<<grid, 256, 0, s>>>(a, (const float *)k, (const float *)v, p(c.k_codes), p(c.k_scales), p(c.v_codes), p(c.v_scales));
+  });
+}
+
 hipError_t mx_rows(const Dims &d, const cca_mx_cache &c, void *k, void *v, int n, const int *first, const int *counts, hipStream_t s) {
-  const StoreArgs a{n, d.Hk, d.dh, d.T, d.T, store_tiles(d, n), first, counts, nullptr, nullptr, nullptr};
+  const StoreArgs a{n, d.Hk, d.T, d.T, store_tiles(d, n), first, counts, nullptr, nullptr, nullptr};
   const unsigned grid = (unsigned)(a.tiles < MAX_GRID ? a.tiles : MAX_GRID);
   auto p = [](void *x) { return static_cast<const unsigned char *>(x); };
-  if (d.bf16) mx_rows_kernel<bf16_t><<<grid, 256, 0, s>>>(a, (bf16_t *)k, (bf16_t *)v, p(c.k_codes), p(c.k_scales), p(c.v_codes), p(c.v_scales));
-  else mx_rows_kernel<float><<<grid, 256, 0, s>>>(a, (float *)k, (float *)v, p(c.k_codes), p(c.k_scales), p(c.v_codes), p(c.v_scales));
-  return hipGetLastError();
+  return by_width(d.dh, [&](auto w) {
+    constexpr int N32 = decltype(w)::value;
+    if (d.bf16) mx_rows_kernel<bf16_t, N32><<<grid, 256, 0, s>>>(a, (bf16_t *)k, (bf16_t *)v, p(c.k_codes), p(c.k_scales), p(c.v_codes), p(c.v_scales));
+    else mx_rows_kernel<float, N32><<<grid, 256, 0, s>>>(a, (float *)k, (float *)v, p(c.k_codes), p(c.k_scales), p(c.v_codes), p(c.v_scales));
+  });
 }
 
 // The plan of an eviction: holes, movers (a budget leaves at most T / 2 moves), counts.
