@@ -66,30 +66,87 @@ __global__ __launch_bounds__(WAVES * 64, (WAVES == 4 ? Form<N32, TERMS>::RESIDEN
   extern __shared__ __attribute__((aligned(16))) float mrg[];  // [WAVES][COLS][STRIDE]
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 15, j = lane >> 4;
   const int split = blockIdx.x % a.nsplit, g = (blockIdx.x / a.nsplit) % a.Hk, b = blockIdx.x / (a.nsplit * a.Hk);
-  const int nr = min(F::COLS, a.R - a.r0);
-  const int len = seq_len(a, b), k_begin = split * a.per, k_end = min(len, k_begin + a.per);
-  if (k_begin >= len && split > 0) return;  // a short sequence has fewer splits: nobody reads the others' place
+  const int nr = min(F::COLS, a.R - a.r0), k_begin = split * a.per;
   const long long head = (long long)b * a.Hk + g;
+  int k0 = k_begin + wave * BLK;
 
-  // q: column m's channels j d_h/4 + 8 s + 0 ... 7, in TERMS parts
+  const unsigned char *const kc = a.k_codes + (head * a.T + k_begin) * (DH / 2) + j * (DH / 8);
+  const unsigned char *const vc = a.v_codes + (head * a.T + k_begin) * (DH / 2) + (PB < 4 ? m * PB : 0);
+  const unsigned char *const ks = a.k_scales + head * N32 * a.T + k_begin, *const vs = a.v_scales + head * N32 * a.T + k_begin;
+  const int rows = a.T - k_begin;  // of this head, from here (k_begin lies below the longest length)
+  int g0 = j * N32 / 4;            // first group of the lane's K channels
+  uint32_t kw[NT][N32], vw[NT * 4][NP], sk[NG], sv[NP][NT];
+  int vp[NP], vg[NP];  // offset of a piece in the row; its group
+#pragma unroll
+  for (int p = 0; p < NP; ++p) {
+    const int dw = 16 * p + m;  // (PB = 4) word of the row; those past it repeat the last, nobody stores their channels
+    vp[p] = PB < 4 ? 0 : 4 * min(dw, 4 * N32 - 1);
+    vg[p] = PB == 1 ? 0 : PB == 2 ? m >> 3 : min(dw, 4 * N32 - 1) >> 2;
+  }
+  auto load_k = [&](int kk) __attribute__((always_inline)) {
+    const int row = min(kk - k_begin + NT * m, rows - NT);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) __builtin_memcpy(kw[t], __builtin_assume_aligned(kc + (uint32_t)(row + t) * (uint32_t)(DH / 2), N32 % 4 == 0 ? 16 : 4 * (N32 & -N32)), 4 * N32);
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      const unsigned char *p = ks + (long long)min(g0 + i, N32 - 1) * a.T + row;
+      if constexpr (NT == 4) sk[i] = *reinterpret_cast<const uint32_t *>(p);
+      else sk[i] = *reinterpret_cast<const uint16_t *>(p);
+    }
+  };
+  auto load_v = [&](int kk) __attribute__((always_inline)) {
+    const int row = min(kk - k_begin + 4 * NT * j, rows - 4 * NT);
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      const unsigned char *sp = vs + (long long)vg[p] * a.T + row;
+      if constexpr (NT == 4) {
+        const mx_u4 w = *reinterpret_cast<const mx_u4 *>(sp);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sv[p][i] = w[i];
+      } else {
+        const mx_u2 w = *reinterpret_cast<const mx_u2 *>(sp);
+        sv[p][0] = w[0], sv[p][1] = w[1];
+      }
+#pragma unroll
+      for (int i = 0; i < 4 * NT; ++i) {
+        const unsigned char *cp = vc + (uint32_t)row * (uint32_t)(DH / 2) + vp[p] + i * (DH / 2);
+        if constexpr (PB == 4) vw[i][p] = *reinterpret_cast<const uint32_t *>(cp);
+        else if constexpr (PB == 2) vw[i][p] = *reinterpret_cast<const uint16_t *>(cp);
+        else vw[i][p] = *cp;
+      }
+    }
+  };
+  // q: column m's channels j d_h/4 + 8 s + 0 ... 7, in TERMS parts.  Parts have to be taken from fp32 numbers, behind the first block's requests.
   const int col = TERMS == 1 ? m & 7 : m;
   const long long hq = (long long)b * a.Hq + g * a.R + a.r0 + min(col, nr - 1);  // columns past the last head repeat it; nobody stores them
   mx_bf8 qf[N32][TERMS == 3 ? 3 : 1];
+  const bool parts = TERMS == 3 || a.q_f32;
+  if (!parts) {
 #pragma unroll
-  for (int s = 0; s < N32; ++s) {
-    const long long at = hq * DH + j * (DH / 4) + 8 * s;
-    if (TERMS < 3 && !a.q_f32) {
-      qf[s][0] = __builtin_bit_cast(mx_bf8, *reinterpret_cast<const mx_u4 *>(static_cast<const bf16_t *>(a.q) + at));
-    } else {
-      const mx_f4 x = *reinterpret_cast<const mx_f4 *>(static_cast<const float *>(a.q) + at), y = *reinterpret_cast<const mx_f4 *>(static_cast<const float *>(a.q) + at + 4);
+    for (int s = 0; s < N32; ++s)
+      qf[s][0] = __builtin_bit_cast(mx_bf8, *reinterpret_cast<const mx_u4 *>(static_cast<const bf16_t *>(a.q) + hq * DH + j * (DH / 4) + 8 * s));
+  }
+  __builtin_amdgcn_sched_barrier(0);
+  // The first block is asked for before the length is known: rows behind it lie inside the capacity, and are dropped below
+  load_k(k0);
+  __builtin_amdgcn_sched_barrier(0);
+  load_v(k0);
+  __builtin_amdgcn_sched_barrier(0);
+  const int len = seq_len(a, b), k_end = min(len, k_begin + a.per);
+  if (k_begin >= len && split > 0) return;  // a short sequence has fewer splits: nobody reads the others' place
+  if (parts) {
+#pragma unroll
+    for (int s = 0; s < N32; ++s) {
+      const float *qp = static_cast<const float *>(a.q) + hq * DH + j * (DH / 4) + 8 * s;
+      const mx_f4 x = *reinterpret_cast<const mx_f4 *>(qp), y = *reinterpret_cast<const mx_f4 *>(qp + 4);
       float r[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
 #pragma unroll
       for (int u = 0; u < (TERMS == 3 ? 3 : 1); ++u) {
         mx_u4 w;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          w[i] = mx_pack(r[2 * i], r[2 * i + 1]);
-          const uint32_t wi = w[i];
+          const uint32_t wi = mx_pack(r[2 * i], r[2 * i + 1]);
+          w[i] = wi;
           r[2 * i] -= mx_lo(wi), r[2 * i + 1] -= mx_hi(wi);
         }
         qf[s][u] = __builtin_bit_cast(mx_bf8, w);
@@ -102,58 +159,7 @@ __global__ __launch_bounds__(WAVES * 64, (WAVES == 4 ? Form<N32, TERMS>::RESIDEN
 #pragma unroll
   for (int t = 0; t < VT; ++t) o[t] = mx_f4{0.f, 0.f, 0.f, 0.f};
 
-  int k0 = k_begin + wave * BLK;
   if (k0 < k_end) {  // wave-uniform
-    const unsigned char *const kc = a.k_codes + (head * a.T + k_begin) * (DH / 2) + j * (DH / 8);
-    const unsigned char *const vc = a.v_codes + (head * a.T + k_begin) * (DH / 2) + (PB < 4 ? m * PB : 0);
-    const unsigned char *const ks = a.k_scales + head * N32 * a.T + k_begin, *const vs = a.v_scales + head * N32 * a.T + k_begin;
-    const int rows = a.T - k_begin;  // of this head, from here
-    int g0 = j * N32 / 4;            // first group of the lane's K channels
-    uint32_t kw[NT][N32], vw[NT * 4][NP], sk[NG], sv[NP][NT];
-    int vp[NP], vg[NP];  // offset of a piece in the row; its group
-#pragma unroll
-    for (int p = 0; p < NP; ++p) {
-      const int dw = 16 * p + m;  // (PB = 4) word of the row; those past it repeat the last, nobody stores their channels
-      vp[p] = PB < 4 ? 0 : 4 * min(dw, 4 * N32 - 1);
-      vg[p] = PB == 1 ? 0 : PB == 2 ? m >> 3 : min(dw, 4 * N32 - 1) >> 2;
-    }
-    auto load_k = [&](int kk) __attribute__((always_inline)) {
-      const int row = min(kk - k_begin + NT * m, rows - NT);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) __builtin_memcpy(kw[t], __builtin_assume_aligned(kc + (uint32_t)(row + t) * (uint32_t)(DH / 2), N32 % 4 == 0 ? 16 : 4 * (N32 & -N32)), 4 * N32);
-#pragma unroll
-      for (int i = 0; i < NG; ++i) {
-        const unsigned char *p = ks + (long long)min(g0 + i, N32 - 1) * a.T + row;
-        if constexpr (NT == 4) sk[i] = *reinterpret_cast<const uint32_t *>(p);
-        else sk[i] = *reinterpret_cast<const uint16_t *>(p);
-      }
-    };
-    auto load_v = [&](int kk) __attribute__((always_inline)) {
-      const int row = min(kk - k_begin + 4 * NT * j, rows - 4 * NT);
-#pragma unroll
-      for (int p = 0; p < NP; ++p) {
-        const unsigned char *sp = vs + (long long)vg[p] * a.T + row;
-        if constexpr (NT == 4) {
-          const mx_u4 w = *reinterpret_cast<const mx_u4 *>(sp);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) sv[p][i] = w[i];
-        } else {
-          const mx_u2 w = *reinterpret_cast<const mx_u2 *>(sp);
-          sv[p][0] = w[0], sv[p][1] = w[1];
-        }
-#pragma unroll
-        for (int i = 0; i < 4 * NT; ++i) {
-          const unsigned char *cp = vc + (uint32_t)row * (uint32_t)(DH / 2) + vp[p] + i * (DH / 2);
-          if constexpr (PB == 4) vw[i][p] = *reinterpret_cast<const uint32_t *>(cp);
-          else if constexpr (PB == 2) vw[i][p] = *reinterpret_cast<const uint16_t *>(cp);
-          else vw[i][p] = *cp;
-        }
-      }
-    };
-    load_k(k0);
-    __builtin_amdgcn_sched_barrier(0);
-    load_v(k0);
-    __builtin_amdgcn_sched_barrier(0);
     float *const sc = a.scores ? a.scores + hq * a.T : nullptr;
 
     auto block = [&](auto last_) __attribute__((always_inline)) {
@@ -485,7 +491,7 @@ Layout layout(const Dims &d) {
   Layout L;
   size_t off = 0;
   auto take = [&](size_t n) { const size_t at = off; off += align256(n); return at; };
-  const size_t splits = (size_t)d.B * d.Hq * mx_max_splits((long long)d.B * d.Hk, d.T, d.dh);
+  const size_t splits = (size_t)d.B * d.Hq * mx_max_splits((long long)d.B * d.Hk, d.T);
   L.state = take(splits * sizeof(mx_f2));
   L.part = take(splits * d.dh * sizeof(float));
   L.scores = take((size_t)d.B * d.Hq * d.T * sizeof(float));

@@ -8,7 +8,7 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 SOURCE = r"""
 #include "cca_rules.h"
 extern "C" {
-int r_max_splits(long long groups, int T, int dh) { return cca::mx_max_splits(groups, T, dh); }
+int r_max_splits(long long groups, int T) { return cca::mx_max_splits(groups, T); }
 void r_split(long long groups, int T, int longest, int dh, int weights, int *out) {
   const cca::MxSplit s = cca::mx_split(groups, T, longest, dh, weights);
   out[0] = s.n, out[1] = s.rows, out[2] = s.many;
@@ -23,8 +23,8 @@ with tempfile.TemporaryDirectory() as tmp:
     _lib = C.CDLL(os.path.join(tmp, "r.so"))
 
 
-def max_splits(groups, T, dh):
-    return _lib.r_max_splits(C.c_longlong(groups), T, dh)
+def max_splits(groups, T):
+    return _lib.r_max_splits(C.c_longlong(groups), T)
 
 
 def split(groups, T, longest, dh, weights):

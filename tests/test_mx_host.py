@@ -189,5 +189,5 @@ def test_splits_fit_the_workspace_and_whole_rounds(groups):
             for longest in {1, 2, T // 3 + 1, T - 1, T}:
                 for weights in (False, True):
                     n, rows, _ = rules_mx.split(groups, T, longest, dh, weights)
-                    assert 1 <= n <= rules_mx.max_splits(groups, T, dh) <= 256 and rows > 0
+                    assert 1 <= n <= rules_mx.max_splits(groups, T) <= 256 and rows > 0
                     assert -(-longest // rows) == n and (n == 1 or rows % (64 if dh <= 128 else 32) == 0)
