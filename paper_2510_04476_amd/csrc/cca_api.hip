@@ -616,7 +616,7 @@ static bool same_or_apart(const void *out, const void *in, size_t bytes) {
 }
 
 struct MxStepLayout {
-  size_t lat, q, k, v, o, attn, total;  // byte offsets
+  size_t lat, q, o, attn, total;  // byte offsets
 };
 static MxStepLayout mx_step_layout(const Dims &d) {
   MxStepLayout L;
@@ -624,8 +624,6 @@ static MxStepLayout mx_step_layout(const Dims &d) {
   auto take = [&](size_t bytes) { size_t o = off; off += align_up(bytes, 256); return o; };
   L.lat = take(d.bf16 ? (size_t)d.B * d.n_lat * sizeof(float) : 0);  // (fp32: the rows go straight into the ring)
   L.q = take((size_t)d.B * d.e_q * sizeof(float));
-  L.k = take((size_t)d.B * d.e_kv * d.esize());
-  L.v = take((size_t)d.B * d.e_kv * d.esize());
   L.o = take((size_t)d.B * d.e_q * d.esize());
   L.attn = take(mx_attention_scratch_bytes(d));
   L.total = off;
@@ -673,7 +671,7 @@ cca_status cca_cache_append_mx(const cca_config *cfg, const cca_mx_cache *cache,
   if (st != CCA_OK) return st;
   if (n < 1 || n > d.T) return CCA_ERR_SHAPE;
   if (!aligned16(k) || !aligned16(v) || !aligned4(rows) || !aligned4(counts) || !aligned4(pos)) return CCA_ERR_ALIGN;
-  return mx_store(d, *cache, k, v, n, rows, d.T, counts, pos, (hipStream_t)hip_stream) == hipSuccess ? CCA_OK : CCA_ERR_LAUNCH;
+  return mx_store(d, *cache, k, v, n, rows, counts, pos, (hipStream_t)hip_stream) == hipSuccess ? CCA_OK : CCA_ERR_LAUNCH;
 }
 
 cca_status cca_cache_rows_mx(const cca_config *cfg, const cca_mx_cache *cache, void *k, void *v, int32_t n, const int32_t *first,
@@ -752,8 +750,7 @@ cca_status cca_decode_step_mx(const cca_config *cfg, const cca_weights *w, const
   const int P = decode_ring_rows(d);
   const RowDest rows{d.n_lat, nullptr, 0, 1}, ring{(long long)P * d.n_lat, pos, POS_MAX, P};
   if (mx_project(d.bf16, x_new, *w_down, d.bf16 ? lat : lat_ring, true, d.bf16 ? rows : ring, d.B, d.E, d.n_lat, s) != hipSuccess ||
-      decode_prologue(d, *w, lat, lat_ring, POS_MAX, pos, q, ws + L.k, ws + L.v, s) != hipSuccess ||
-      mx_store(d, *cache, ws + L.k, ws + L.v, 1, len, max_len, nullptr, pos, s) != hipSuccess ||
+      decode_prologue_mx(d, *w, lat, lat_ring, POS_MAX, pos, q, *cache, len, max_len, s) != hipSuccess ||
       mx_attention(d, *cache, q, true, len, max_len, 1, ws + L.o, nullptr, cache->weight, cache->weight, ws + L.attn, s) != hipSuccess ||
       mx_project(d.bf16, ws + L.o, *w_out, out, false, RowDest{d.E, nullptr, 0, 1}, d.B, d.e_q, d.E, s) != hipSuccess)
     return CCA_ERR_LAUNCH;

@@ -12,6 +12,7 @@
 #include <type_traits>
 
 #include "cca_internal.h"
+#include "cca_mx.h"
 
 namespace cca {
 
@@ -26,7 +27,15 @@ struct DecArgs {
   uint32_t flags;
   float rope_base, scale, norm_eps;
   const int *pos_seq;  // per-sequence positions (device, B entries) or null: every sequence at `pos`
-  bool one_row;        // the new key and value are the only row of `S` = 1 rows, whatever the position
+};
+
+// A 4-bit cache in the place of k_cache, v_cache: the new row of sequence b is clamp(rows[b], 0, max_row)
+struct MxDest {
+  unsigned char *k_codes, *k_scales, *v_codes, *v_scales;
+  int *row_pos;   // may be null
+  float *weight;  // may be null
+  const int *rows;
+  int max_row;
 };
 
 // Position of sequence b's new token.  With per-sequence positions `pos` is the largest one the host vouched for
@@ -170,14 +179,15 @@ __device__ __forceinline__ float dpp_add(float x) {
   return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
 }
 
-template <typename T, int CH, int LPO, int NP>
+template <typename T, int CH, int LPO, int NP, bool MX>
 __global__ __launch_bounds__(512) void decode_prologue_kernel(DecArgs a, T *__restrict__ hist, const float *__restrict__ part,
                                                              int nparts, const T *__restrict__ w0, const T *__restrict__ w1,
                                                              const float *__restrict__ temp, float *__restrict__ q_new,
-                                                             T *__restrict__ k_cache, T *__restrict__ v_cache) {
+                                                             T *__restrict__ k_cache, T *__restrict__ v_cache, MxDest mx) {
   extern __shared__ __attribute__((aligned(16))) float sm[];  // y0[dh][k_ch] | yrot[dh] | cos[dh/2] | sin[dh/2]
   const int b = blockIdx.x, head = blockIdx.y, dh = a.dh, tid = threadIdx.x, t = seq_pos(a, b);
-  const long long crow = (long long)b * a.S + (a.one_row ? 0 : t);  // cache row of the new token
+  const long long crow = (long long)b * a.S + t;  // cache row of the new token
+  const int mx_row = MX ? mx_clamp(mx.rows[b], 0, mx.max_row) : 0;
   T *const slot = hist + ((long long)b * a.P + t % a.P) * a.n_lat;
   // (fp32: the projection wrote the rows into the ring itself)
   const NewRow<T, NP> now{std::is_same<T, float>::value ? reinterpret_cast<const float *>(slot) : part + (long long)b * a.n_lat,
@@ -194,7 +204,12 @@ __global__ __launch_bounds__(512) void decode_prologue_kernel(DecArgs a, T *__re
       float val;
       if (c < a.v_half || !(a.flags & CCA_V_SHIFT)) val = cur;
       else val = prev ? load_f(prev + c) : 0.f;
-      store_f(v_cache + crow * a.e_kv + c, val);
+      if constexpr (MX) {  // (d_h is a multiple of 32 and at most the number of threads: one channel each)
+        const long long gh = (long long)b * a.Hk + g;
+        mx_put(val, i, mx.v_codes + (gh * a.S + mx_row) * (dh / 2), mx.v_scales + gh * (dh / 32) * a.S + mx_row, a.S);
+      } else {
+        store_f(v_cache + crow * a.e_kv + c, val);
+      }
     }
     return;
   }
@@ -366,6 +381,15 @@ __global__ __launch_bounds__(512) void decode_prologue_kernel(DecArgs a, T *__re
       T tmp;
       store_f(&tmp, y);
       q_new[((long long)b * a.Hq + head) * dh + o] = load_f(&tmp);
+    } else if constexpr (MX) {
+      const long long gh = (long long)b * a.Hk + head - a.Hq;
+      T tmp;
+      store_f(&tmp, y);  // as it would be cached
+      mx_put(load_f(&tmp), o, mx.k_codes + (gh * a.S + mx_row) * (dh / 2), mx.k_scales + gh * (dh / 32) * a.S + mx_row, a.S);
+      if (o == 0) {
+        if (mx.row_pos) mx.row_pos[gh * a.S + mx_row] = a.pos_seq[b];
+        if (mx.weight) mx.weight[gh * a.S + mx_row] = 0.f;
+      }
     } else {
       store_f(k_cache + crow * a.e_kv + (head - a.Hq) * dh + o, y);
     }
@@ -1183,20 +1207,21 @@ DecLayout layout(const Dims &d) {
   return L;
 }
 
-template <typename T>
+template <typename T, bool MX = false>
 hipError_t prologue_t(const Dims &d, const cca_weights &w, const DecArgs &a, const float *gpart, int nparts, void *hist, float *q_new, void *k_cache,
-                      void *v_cache, hipStream_t s) {
+                      void *v_cache, hipStream_t s, const MxDest &mx = MxDest{}) {
   const int kc = (d.flags & CCA_CONV_CH) ? d.k_ch : 1;
   const int threads = d.dh <= 64 ? 256 : 512, per_lane = (d.dh * kc / 8 + 7) / 8;  // filter chunks per lane of 8
   const size_t smem = sizeof(float) * ((size_t)kc * d.dh + 2 * d.dh);
+  constexpr bool ONE = MX || std::is_same<T, float>::value;  // never more parts than one
 #define CCA_DEC_PRO_NP(CH, LPO, NP)                                                                                       \
-  decode_prologue_kernel<T, CH, LPO, NP><<<dim3(d.B, d.Hq + 2 * d.Hk), threads, smem, s>>>(                                \
-      a, (T *)hist, gpart, nparts, (const T *)w.w_conv_seq, (const T *)w.w_conv_ch, w.temp, q_new, (T *)k_cache, (T *)v_cache)
+  decode_prologue_kernel<T, CH, LPO, NP, MX><<<dim3(d.B, d.Hq + 2 * d.Hk), threads, smem, s>>>(                            \
+      a, (T *)hist, gpart, nparts, (const T *)w.w_conv_seq, (const T *)w.w_conv_ch, w.temp, q_new, (T *)k_cache, (T *)v_cache, mx)
 #define CCA_DEC_PRO(CH, LPO)                                                                                              \
-  if (std::is_same<T, float>::value || nparts == 1) CCA_DEC_PRO_NP(CH, LPO, 1);                                            \
-  else if (nparts == 2) CCA_DEC_PRO_NP(CH, LPO, (std::is_same<T, float>::value ? 1 : 2));                                  \
-  else if (nparts <= 5) CCA_DEC_PRO_NP(CH, LPO, (std::is_same<T, float>::value ? 1 : 5));                                  \
-  else CCA_DEC_PRO_NP(CH, LPO, (std::is_same<T, float>::value ? 1 : MAX_PARTS))
+  if (ONE || nparts == 1) CCA_DEC_PRO_NP(CH, LPO, 1);                                                                      \
+  else if (nparts == 2) CCA_DEC_PRO_NP(CH, LPO, (ONE ? 1 : 2));                                                            \
+  else if (nparts <= 5) CCA_DEC_PRO_NP(CH, LPO, (ONE ? 1 : 5));                                                            \
+  else CCA_DEC_PRO_NP(CH, LPO, (ONE ? 1 : MAX_PARTS))
   if (per_lane <= 2) { CCA_DEC_PRO(2, 8); }
   else if (per_lane <= 4) { CCA_DEC_PRO(4, 8); }
   else if (per_lane <= 8) { CCA_DEC_PRO(8, 8); }
@@ -1213,7 +1238,7 @@ hipError_t step_t(const Dims &d, const cca_weights &w, const void *x_new, void *
   const DecLayout L = layout(d);
   const int P = ring_rows(d);
   DecArgs a{d.B, d.T, d.Hq, d.Hk, d.dh, d.R, d.e_q, d.e_kv, d.n_lat, d.v_half, d.k_seq, d.k_ch, P, pos,
-            d.flags, d.rope_base, d.scale, d.norm_eps, pos_seq, false};
+            d.flags, d.rope_base, d.scale, d.norm_eps, pos_seq};
   float *q_new = reinterpret_cast<float *>(ws + L.q_new);
   T *o = reinterpret_cast<T *>(ws + L.o);
   float *part = reinterpret_cast<float *>(ws + L.part);
@@ -1306,11 +1331,14 @@ hipError_t decode_step(const Dims &d, const cca_weights &w, const void *x_new, v
                 : step_t<float>(d, w, x_new, k_cache, v_cache, hist, pos, pos_seq, out, ws, s);
 }
 
-hipError_t decode_prologue(const Dims &d, const cca_weights &w, const float *lat, void *hist, int pos, const int *pos_seq, float *q, void *k,
-                           void *v, hipStream_t s) {
-  const DecArgs a{d.B, 1, d.Hq, d.Hk, d.dh, d.R, d.e_q, d.e_kv, d.n_lat, d.v_half, d.k_seq, d.k_ch, ring_rows(d), pos,
-                  d.flags, d.rope_base, d.scale, d.norm_eps, pos_seq, true};
-  return d.bf16 ? prologue_t<bf16_t>(d, w, a, lat, 1, hist, q, k, v, s) : prologue_t<float>(d, w, a, lat, 1, hist, q, k, v, s);
+hipError_t decode_prologue_mx(const Dims &d, const cca_weights &w, const float *lat, void *hist, int max_pos, const int *pos, float *q,
+                              const cca_mx_cache &cache, const int *rows, int max_row, hipStream_t s) {
+  const DecArgs a{d.B, d.T, d.Hq, d.Hk, d.dh, d.R, d.e_q, d.e_kv, d.n_lat, d.v_half, d.k_seq, d.k_ch, ring_rows(d), max_pos,
+                  d.flags, d.rope_base, d.scale, d.norm_eps, pos};
+  auto p = [](void *x) { return static_cast<unsigned char *>(x); };
+  const MxDest mx{p(cache.k_codes), p(cache.k_scales), p(cache.v_codes), p(cache.v_scales), reinterpret_cast<int *>(cache.pos), cache.weight, rows, max_row};
+  return d.bf16 ? prologue_t<bf16_t, true>(d, w, a, lat, 1, hist, q, nullptr, nullptr, s, mx)
+                : prologue_t<float, true>(d, w, a, lat, 1, hist, q, nullptr, nullptr, s, mx);
 }
 
 }  // namespace cca

@@ -222,19 +222,19 @@ size_t decode_scratch_bytes(const Dims &d);
 // sequence takes its own (clamped to [0, pos] in the kernels)
 hipError_t decode_step(const Dims &d, const cca_weights &w, const void *x_new, void *k_cache, void *v_cache, void *hist,
                        int pos, const int *pos_seq, void *out, void *workspace, hipStream_t s);
-// The transforms of the new token alone: from the fp32 rows of the down-projection (`lat`, (B, N_lat); fp32 storage: the rows are in the
-// ring already) to q (fp32 of the storage type's values, (B, H_q, d_h)) and k, v (B, H_k, d_h); the ring gets the new rows.
-hipError_t decode_prologue(const Dims &d, const cca_weights &w, const float *lat, void *hist, int pos, const int *pos_seq, float *q, void *k,
-                           void *v, hipStream_t s);
+// The transforms of the new token alone, for a 4-bit cache: from the fp32 rows of the down-projection (`lat`, (B, N_lat); fp32 storage: the
+// rows are in the ring already) to q (fp32 of the storage type's values, (B, H_q, d_h)); the ring gets the new rows, the cache the new key
+// and value (as cca_cache_append_mx stores them) as row clamp(rows[b], 0, max_row), with its position and weight 0 where the cache has them.
+hipError_t decode_prologue_mx(const Dims &d, const cca_weights &w, const float *lat, void *hist, int max_pos, const int *pos, float *q,
+                              const cca_mx_cache &cache, const int *rows, int max_row, hipStream_t s);
 
 // ---- 4-bit serving (include/cca.h) --------------------------------------------
 // bf16: of x and (unless y_f32) y; else both are fp32
 hipError_t mx_project(bool bf16, const void *x, const cca_mx_weight &w, void *y, bool y_f32, const RowDest &dest, int M, int K, int N,
                       hipStream_t s);
 hipError_t mx_quantize(bool bf16, const void *w, int K, int N, void *codes, void *scales, hipStream_t s);
-// rows[b] is clamped to [0, max_row]
-hipError_t mx_store(const Dims &d, const cca_mx_cache &c, const void *k, const void *v, int n, const int *rows, int max_row,
-                    const int *counts, const int *pos, hipStream_t s);
+hipError_t mx_store(const Dims &d, const cca_mx_cache &c, const void *k, const void *v, int n, const int *rows, const int *counts,
+                    const int *pos, hipStream_t s);
 hipError_t mx_rows(const Dims &d, const cca_mx_cache &c, void *k, void *v, int n, const int *first, const int *counts, hipStream_t s);
 size_t mx_evict_scratch_bytes(const Dims &d);
 hipError_t mx_evict(const Dims &d, const cca_mx_cache &c, int *len, int max_len, int budget, int recent, float *weight_out, int *pos_out,

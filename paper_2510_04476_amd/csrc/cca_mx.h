@@ -100,6 +100,20 @@ __device__ __forceinline__ float mx_xor16_max(float x) {
   return fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
 }
 
+// Stores one row of a head from one channel to a lane: `o` is this lane's, 32 lanes in a row hold a group, y its number (of the storage type).
+__device__ __forceinline__ void mx_put(float y, int o, unsigned char *codes, unsigned char *scales, long long group_stride) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  float a = mx_max_abs(y, mx_dpp<0xB1>(y));  // quad_perm [1,0,3,2]
+  a = mx_max_abs(a, mx_dpp<0x4E>(a));        // quad_perm [2,3,0,1]
+  a = mx_max_abs(a, mx_dpp<0x141>(a));       // row_half_mirror
+  a = mx_max_abs(a, mx_dpp<0x140>(a));       // row_mirror
+  a = mx_max_abs(a, __shfl_xor(a, 16));
+  const uint32_t s = mx_scale_of(a), byte = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, y, mx_dpp<0xB1>(y), __uint_as_float(s << 23), 0);
+  if ((o & 1) == 0) codes[o >> 1] = s == 255u ? 0 : (unsigned char)byte;
+  if ((o & 31) == 0) scales[(o >> 5) * group_stride] = (unsigned char)s;
+#endif
+}
+
 __device__ __forceinline__ int mx_clamp(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
 
 }  // namespace cca

@@ -16,7 +16,7 @@ constexpr int TOK = 64;  // tokens of a workgroup
 // side by side: they go through LDS so that a wavefront stores them along the tokens.
 // ---------------------------------------------------------------------------
 struct StoreArgs {
-  int n, Hk, T, max_row;
+  int n, Hk, T;
   long long tiles;  // B * 2 H_k * ceil(n / 64): K's heads of a sequence, then V's
 
   const int *rows, *counts, *pos;
@@ -61,7 +61,7 @@ __device__ __forceinline__ Tile tile_of(const StoreArgs &a, long long tile) {
   t.b = (int)(tile / per / (2 * a.Hk));
   t.is_v = hv >= a.Hk;
   t.head = (long long)t.b * a.Hk + hv % a.Hk;
-  t.row0 = a.rows ? mx_clamp(a.rows[t.b], 0, a.max_row) : 0;
+  t.row0 = a.rows ? mx_clamp(a.rows[t.b], 0, a.T) : 0;
   t.live = min(mx_clamp(a.counts ? a.counts[t.b] : a.n, 0, a.n), a.T - t.row0);
   return t;
 }
@@ -431,9 +431,9 @@ static hipError_t by_width(int dh, F f) {
   return hipGetLastError();
 }
 
-hipError_t mx_store(const Dims &d, const cca_mx_cache &c, const void *k, const void *v, int n, const int *rows, int max_row,
-                    const int *counts, const int *pos, hipStream_t s) {
-  const StoreArgs a{n, d.Hk, d.T, max_row, store_tiles(d, n), rows, counts, pos, reinterpret_cast<int *>(c.pos), c.weight};
+hipError_t mx_store(const Dims &d, const cca_mx_cache &c, const void *k, const void *v, int n, const int *rows, const int *counts,
+                    const int *pos, hipStream_t s) {
+  const StoreArgs a{n, d.Hk, d.T, store_tiles(d, n), rows, counts, pos, reinterpret_cast<int *>(c.pos), c.weight};
   const unsigned grid = (unsigned)(a.tiles < MAX_GRID ? a.tiles : MAX_GRID);
   auto p = [](void *x) { return static_cast<unsigned char *>(x); };
   return by_width(d.dh, [&](auto w) {
@@ -444,7 +444,7 @@ hipError_t mx_store(const Dims &d, const cca_mx_cache &c, const void *k, const v
 }
 
 hipError_t mx_rows(const Dims &d, const cca_mx_cache &c, void *k, void *v, int n, const int *first, const int *counts, hipStream_t s) {
-  const StoreArgs a{n, d.Hk, d.T, d.T, store_tiles(d, n), first, counts, nullptr, nullptr, nullptr};
+  const StoreArgs a{n, d.Hk, d.T, store_tiles(d, n), first, counts, nullptr, nullptr, nullptr};
   const unsigned grid = (unsigned)(a.tiles < MAX_GRID ? a.tiles : MAX_GRID);
   auto p = [](void *x) { return static_cast<const unsigned char *>(x); };
   return by_width(d.dh, [&](auto w) {

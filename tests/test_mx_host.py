@@ -191,3 +191,15 @@ def test_splits_fit_the_workspace_and_whole_rounds(groups):
                     n, rows, _ = rules_mx.split(groups, T, longest, dh, weights)
                     assert 1 <= n <= rules_mx.max_splits(groups, T) <= 256 and rows > 0
                     assert -(-longest // rows) == n and (n == 1 or rows % (64 if dh <= 128 else 32) == 0)
+
+
+def test_config_reference_follows_its_fields_and_the_ring_depth_is_the_librarys():
+    cfg = good()
+    assert cfg.ref() is cfg.ref() and cfg.ref()._obj.T == 64
+    cfg.T = 96
+    assert cfg.ref()._obj.T == 96
+    for flags in (B.CCA_FLAGS_PAPER, B.CCA_FLAGS_MHA, B.CCA_FLAGS_PAPER & ~B.CCA_CONV_CH):
+        for k_seq in (1, 2, 4):
+            for k_ch in (1, 3):
+                cfg.flags, cfg.k_seq, cfg.k_ch = flags, k_seq, k_ch
+                assert cfg.ring_rows() == P.cca_decode_workspace_size(cfg)[1]
