@@ -31,6 +31,20 @@ struct AttnArgs {
 // 2^(m - M) for a part's maximum m and sum l; a part without rows has none
 __device__ __forceinline__ float rescale(float m, float l, float M) { return m == -INFINITY && l == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - M); }
 
+// Weights of rows row ... row + 3 of a head: what they had (below `old`: a step's new rows start from 0) plus what they got; rows
+// from len on are left alone
+__device__ __forceinline__ void store_weights(float *weight, int row, int len, int old, mx_f4 before, mx_f4 sum) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sum[i] += row + i < old ? before[i] : 0.f;
+  if (row + 4 <= len) {
+    *reinterpret_cast<mx_f4 *>(weight + row) = sum;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (row + i < len) weight[row + i] = sum[i];
+  }
+}
+
 __device__ __forceinline__ int seq_len(const AttnArgs &a, int b) { return mx_clamp(a.len[b], 0, a.max_len) + a.extra; }
 
 // ---------------------------------------------------------------------------
@@ -64,6 +78,7 @@ __global__ __launch_bounds__(WAVES * 64, (WAVES == 4 ? Form<N32, TERMS>::RESIDEN
   typedef Form<N32, TERMS> F;
   constexpr int DH = F::DH, NT = F::NT, BLK = F::BLK, PB = F::PB, NP = F::NP, VT = F::VT, NG = F::NG;
   extern __shared__ __attribute__((aligned(16))) float mrg[];  // [WAVES][COLS][STRIDE]
+  __shared__ float top[F::COLS], inv[F::COLS];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 15, j = lane >> 4;
   const int split = blockIdx.x % a.nsplit, g = (blockIdx.x / a.nsplit) % a.Hk, b = blockIdx.x / (a.nsplit * a.Hk);
   const int nr = min(F::COLS, a.R - a.r0), k_begin = split * a.per;
@@ -336,7 +351,22 @@ __global__ __launch_bounds__(WAVES * 64, (WAVES == 4 ? Form<N32, TERMS>::RESIDEN
       if constexpr (TERMS == 3) static_cast<float *>(a.o)[h * DH + ch] = res;
       else store_f(static_cast<bf16_t *>(a.o) + h * DH + ch, res);
       if (ch == 0 && a.lse) a.lse[h] = (M + log2f(L)) * 0.69314718055994530942f;
+      if (ch == 0) top[r] = M == -INFINITY ? 0.f : M, inv[r] = L == 0.f ? 0.f : 1.f / L;
     }
+  }
+  if (a.state || !a.weight_out) return;
+  // A head of one workgroup: its weights from the scores that these wavefronts have stored (behind the barriers; read here first)
+  __syncthreads();
+  const float *const mine = a.scores + ((long long)b * a.Hq + g * a.R) * a.T;
+  for (int row = 4 * tid; row < len; row += 4 * WAVES * 64) {
+    mx_f4 sum = {0.f, 0.f, 0.f, 0.f}, before = sum;
+    if (a.weight_in) before = *reinterpret_cast<const mx_f4 *>(a.weight_in + head * a.T + row);
+    for (int r = 0; r < nr; ++r) {
+      const mx_f4 s = *reinterpret_cast<const mx_f4 *>(mine + (long long)r * a.T + row);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[i] = fmaf(__builtin_amdgcn_exp2f(s[i] - top[r]), inv[r], sum[i]);
+    }
+    store_weights(a.weight_out + head * a.T, row, len, len - a.extra, before, sum);
   }
 }
 
@@ -443,16 +473,7 @@ __global__ __launch_bounds__(256) void mx_finish_kernel(AttnArgs a, int dh, long
           }
       }
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) sum[i] += row + i < old ? before[i] : 0.f;
-    float *const to = a.weight_out + head * a.T + row;
-    if (row + 4 <= len) {
-      *reinterpret_cast<mx_f4 *>(to) = sum;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (row + i < len) to[i] = sum[i];
-    }
+    store_weights(a.weight_out + head * a.T, row, len, old, before, sum);
   }
 }
 
@@ -509,8 +530,10 @@ hipError_t mx_attention(const Dims &d, const cca_mx_cache &c, const void *q, boo
   unsigned char *ws = static_cast<unsigned char *>(workspace);
   const int longest = max_len + extra;
   const long long groups = (long long)d.B * d.Hk;
-  const MxSplit split = mx_split(groups, d.T, longest, d.dh, weight_out != nullptr);
-  const bool finish = split.n > 1 || weight_out;
+  // More heads to a group than one pass takes: their weights need a second launch, whatever the splits
+  const bool passes = d.R > 16;
+  const MxSplit split = mx_split(groups, d.T, longest, d.dh, weight_out && passes);
+  const bool finish = split.n > 1 || (weight_out && passes);
   auto p = [](const void *x) { return static_cast<const unsigned char *>(x); };
   AttnArgs a{d.B, d.T, d.Hq, d.Hk, d.R, max_len, extra, split.n, split.rows, 0, d.scale * 1.44269504088896340736f, len, q, q_f32 || !d.bf16,
              p(c.k_codes), p(c.k_scales), p(c.v_codes), p(c.v_scales), finish ? reinterpret_cast<mx_f2 *>(ws + L.state) : nullptr,
