@@ -353,7 +353,7 @@ cca_status cca_mx_workspace_size(const cca_config *cfg, size_t *bytes);
 cca_status cca_mx_quantize(const void *w, int32_t K, int32_t N, int32_t dtype, void *codes, void *scales, void *hip_stream);
 
 /* y (M, N) = x (M, K) W; x and y of type dtype, sums in fp32, any M >= 1 and N >= 1 up to 65536 each.  The 4-bit form of
- * cca_down_project / cca_up_project, meant for the few rows of a decode step. */
+ * cca_down_project / cca_up_project, meant for the few rows of a decode step.  y must not overlap x (CCA_ERR_UNSUPPORTED). */
 cca_status cca_project_mx(const void *x, const cca_mx_weight *w, void *y, int32_t M, int32_t K, int32_t N, int32_t dtype,
                           void *hip_stream);
 
@@ -371,30 +371,31 @@ cca_status cca_cache_rows_mx(const cca_config *cfg, const cca_mx_cache *cache, v
 /* Attention of one new token per sequence: o (B, H_q*d_h) = softmax(scale * q K^T) V over rows 0..len[b]-1 of the cache, q
  * (B, H_q, d_h), query head h reading KV head h / R.  len[b] is clamped to [0, max_len], 0 <= max_len <= T (CCA_ERR_SHAPE).
  * A sequence of length 0 gives o = 0.  lse (B, H_q) fp32 may be NULL: the natural logarithm of the sum of exponentials, -inf
- * for length 0.  weight_out (B, H_k, T) fp32 may be NULL: for each row below len[b] the attention probabilities of the
- * R query heads are added to weight_in (NULL: to 0; weight_out itself: in place; any other overlap is
- * CCA_ERR_UNSUPPORTED); rows from len[b] on are left as they were.  Probabilities enter the product with V with 16 bits or more of mantissa. */
+ * for length 0.  o must not overlap q (CCA_ERR_UNSUPPORTED).  weight_out (B, H_k, T) fp32 may be NULL: for each row below
+ * len[b] the attention probabilities of the R query heads are added to weight_in (NULL: to 0; weight_out itself: in place;
+ * any other overlap is CCA_ERR_UNSUPPORTED); rows from len[b] on are left as they were.  Probabilities enter the product
+ * with V with 16 bits or more of mantissa. */
 cca_status cca_decode_attention_mx(const cca_config *cfg, const cca_mx_cache *cache, const void *q, const int32_t *len,
                                    int32_t max_len, void *o, float *lse, const float *weight_in, float *weight_out,
                                    void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* Keeps at most `budget` rows of every head, 1 <= budget <= T, 0 <= recent <= budget (CCA_ERR_SHAPE).  Of the n = len[b]
- * rows of a (sequence, head) with n > budget stay the `budget` of highest rank: first the rows whose position exceeds the head's
- * largest one less `recent`, then by weight, the greater first (a NaN last), and of equal ones the lower row.  The kept rows that lie
- * at or beyond `budget` move, in order, into the places of the rows that went, in order; every other kept row
- * stays where it is, so that rows 0..budget-1 are the cache afterwards, in no order of position.  What lies beyond is undefined.
- * Needs cache->pos and cache->weight.  pos_out, weight_out (B, H_k, T) and len_out (B) get the new positions, weights and lengths
- * min(len[b], budget); NULL or the input itself: in place.  Apart from their input (any other overlap is CCA_ERR_UNSUPPORTED) their entries from
- * the new length on are left as they were and the input is only read. */
+ * rows of a (sequence, head) with n > budget stay the `budget` of highest rank: first the rows whose position exceeds the
+ * head's largest one less `recent` (all alike), then by weight, the greater first (a NaN last), and of equal ones the lower
+ * row.  The kept rows that lie at or beyond `budget` move, in order, into the places of the rows that went, in order; every
+ * other kept row stays where it is, so that rows 0..budget-1 are the cache afterwards, in no order of position.  What lies
+ * beyond is undefined.  Needs cache->pos and cache->weight.  pos_out, weight_out (B, H_k, T) and len_out (B) get the new
+ * positions, weights and lengths min(len[b], budget); NULL or the input itself: in place.  Apart from their input (any other
+ * overlap is CCA_ERR_UNSUPPORTED) their entries from the new length on are left as they were and the input is only read. */
 cca_status cca_cache_evict_mx(const cca_config *cfg, const cca_mx_cache *cache, int32_t *len, int32_t max_len, int32_t budget,
                               int32_t recent, float *weight_out, int32_t *pos_out, int32_t *len_out, void *workspace,
                               size_t workspace_bytes, void *hip_stream);
 
 /* cca_decode_step_ragged over a 4-bit cache and 4-bit projections.  Sequence b's new token stands at position pos[b] of its
- * text (rotary angle, ring slot; clamped to [0, 2^30]) and becomes row len[b] of every head (clamped to [0, max_len], 0 <= max_len < T, else
- * CCA_ERR_SHAPE): with rows evicted, len[b] is below pos[b].  Its keys and values are stored as cca_cache_append_mx stores them, then
- * it attends to rows 0..len[b], its own included, as read back.  With cache->weight every row's weight grows by the attention it got, the new row's from
- * 0; with cache->pos the new row's position is recorded.  pos and len are not advanced.  w_down (E, N_lat) and w_out (e_q, E) are the
+ * text (rotary angle, ring slot; clamped to [0, 2^30]) and becomes row len[b] of every head (clamped to [0, max_len],
+ * 0 <= max_len < T, else CCA_ERR_SHAPE): with rows evicted, len[b] is below pos[b].  Its keys and values are stored as
+ * cca_cache_append_mx stores them, then it attends to rows 0..len[b], its own included, as read back.  With cache->weight
+ * every row's weight grows by the attention it got, the new row's from 0; with cache->pos the new row's position is recorded, pos[b] as it is.  pos and len are not advanced.  w_down (E, N_lat) and w_out (e_q, E) are the
  * weights of cca_weights in 4 bits (E and e_q multiples of 32); of `w` the members w_conv_seq, w_conv_ch and temp are
  * read.  lat_ring: as in cca_decode_state. */
 cca_status cca_decode_step_mx(const cca_config *cfg, const cca_weights *w, const cca_mx_weight *w_down, const cca_mx_weight *w_out,

@@ -156,6 +156,9 @@ class CCAConfig:
         object.__setattr__(self, name, value)
         self.__dict__.pop("_kept", None)
 
+    def __getstate__(self):  # (copies and pickles make their own C form)
+        return {k: v for k, v in self.__dict__.items() if k != "_kept"}
+
     def ref(self):
         """The C form by reference, made again after a field has changed."""
         kept = self.__dict__.get("_kept")
@@ -559,8 +562,17 @@ class CCAMXWeight:
             raise ValueError(f"codes: {tuple(self.codes.shape)}, expected (N, K/2)")
         n, k, index = self.codes.shape[0], 2 * self.codes.shape[1], self.codes.get_device()
         c = cca_mx_weight(_mx_ptr("codes", self.codes, (n, k // 2), torch.uint8, index), _mx_ptr("scales", self.scales, (n, k // 32), torch.uint8, index))
-        for name, v in (("K", k), ("N", n), ("_index", index), ("_c", c), ("_ref", C.byref(c))):
+        for name, v in (("K", k), ("N", n), ("_index", index), ("_at", (c.codes, c.scales)), ("_c", c), ("_kept", C.byref(c))):
             object.__setattr__(self, name, v)
+
+    def __reduce__(self):
+        return CCAMXWeight, (self.codes, self.scales)
+
+    def ref(self):
+        """The C form by reference, made again where a tensor has got another storage."""
+        if (self.codes.data_ptr(), self.scales.data_ptr()) != self._at:
+            self.__post_init__()
+        return self._kept
 
 
 @dataclass(frozen=True)
@@ -584,8 +596,17 @@ class CCAMXCache:
                                 ("pos", (B, Hk, T), torch.int32), ("weight", (B, Hk, T), torch.float32)):
             ptrs[name] = _mx_opt(name, getattr(self, name), shape, dt, index)
         c = cca_mx_cache(**ptrs)
-        for name, v in (("_index", index), ("_device", self.k_codes.device), ("_layout", (B, Hk, T, 2 * half)), ("_c", c), ("_ref", C.byref(c))):
+        for name, v in (("_index", index), ("_device", self.k_codes.device), ("_layout", (B, Hk, T, 2 * half)), ("_at", self._now()), ("_c", c),
+                        ("_kept", C.byref(c))):
             object.__setattr__(self, name, v)
+
+    def __reduce__(self):
+        return CCAMXCache, (self.k_codes, self.k_scales, self.v_codes, self.v_scales, self.pos, self.weight)
+
+    def _now(self):
+        pos, weight = self.pos, self.weight
+        return (self.k_codes.data_ptr(), self.k_scales.data_ptr(), self.v_codes.data_ptr(), self.v_scales.data_ptr(),
+                None if pos is None else pos.data_ptr(), None if weight is None else weight.data_ptr())
 
     @staticmethod
     def allocate(cfg: CCAConfig, device, with_weights: bool = True) -> "CCAMXCache":
@@ -598,7 +619,10 @@ class CCAMXCache:
     def _for(self, cfg: CCAConfig):
         if self._layout != (cfg.B, cfg.n_kv_heads, cfg.T, cfg.head_dim):
             raise ValueError(f"cache of (B, H_k, T, d_h) = {self._layout}, config of {(cfg.B, cfg.n_kv_heads, cfg.T, cfg.head_dim)}")
-        return self._ref
+        if self._now() != self._at:  # a tensor has got another storage
+            self.__post_init__()
+            return self._for(cfg)
+        return self._kept
 
 
 def cca_mx_workspace_size(cfg: CCAConfig) -> int:
@@ -631,7 +655,7 @@ def cca_project_mx(x: torch.Tensor, w: CCAMXWeight, out: torch.Tensor | None = N
     y_shape = (*shape[:-1], w.N)
     x_ptr = _mx_ptr("x", x, shape, dt, index)
     out, out_ptr = _mx_out("out", out, y_shape, dt, index, x)
-    _mx_call("cca_project_mx", index, x_ptr, w._ref, out_ptr, x.numel() // w.K, w.K, w.N, CCA_BF16 if dt is torch.bfloat16 else CCA_F32)
+    _mx_call("cca_project_mx", index, x_ptr, w.ref(), out_ptr, x.numel() // w.K, w.K, w.N, CCA_BF16 if dt is torch.bfloat16 else CCA_F32)
     return out
 
 
@@ -705,6 +729,8 @@ class CCADecodeStateMX:
 
     def load_prefill(self, cfg: CCAConfig, saved: CCASaved, n_tokens: int) -> None:
         """Stores the first n_tokens of a prefill's saved k, v and takes over the last rows of its lat."""
+        if n_tokens == 0:
+            return
         zero = torch.zeros(cfg.B, dtype=torch.int32, device=self.lat_ring.device)
         cca_cache_append_mx(cfg, self.cache, saved.k[:, :n_tokens].contiguous(), saved.v[:, :n_tokens].contiguous(), zero)
         P_ = self.lat_ring.shape[1]
@@ -723,7 +749,7 @@ def cca_decode_step_mx(cfg: CCAConfig, w: CCAWeights, w_down: CCAMXWeight, w_out
         if q.K != k or q.N != n or q._index != index:
             raise ValueError(f"{name}: of (K, N) = {(q.K, q.N)} on {q.codes.device}, expected {(k, n)} on {state.cache._device}")
     cw, ring = w.c(), (B, cfg.ring_rows(), cfg.n_lat)
-    _mx_call("cca_decode_step_mx", index, cfg.ref(), C.byref(cw), w_down._ref, w_out._ref, _mx_ptr("x_new", x_new, x_shape, dt, index),
+    _mx_call("cca_decode_step_mx", index, cfg.ref(), C.byref(cw), w_down.ref(), w_out.ref(), _mx_ptr("x_new", x_new, x_shape, dt, index),
              state.cache._for(cfg), _mx_ptr("lat_ring", state.lat_ring, ring, dt, index), _mx_ptr("pos", pos, per_seq, torch.int32, index),
              _mx_ptr("lens", lens, per_seq, torch.int32, index), max_len, out_ptr,
              _mx_ptr("workspace", ws, ws.shape, torch.uint8, index), ws.numel())

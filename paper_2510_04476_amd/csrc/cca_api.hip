@@ -656,6 +656,8 @@ cca_status cca_project_mx(const void *x, const cca_mx_weight *w, void *y, int32_
   cca_status st = mx_weight_check(w);
   if (st != CCA_OK) return st;
   if (!aligned16(x) || !aligned16(y)) return CCA_ERR_ALIGN;
+  const size_t es = dtype == CCA_BF16 ? 2 : 4;
+  if (overlap(x, (size_t)M * K * es, y, (size_t)M * N * es)) return CCA_ERR_UNSUPPORTED;
   return mx_project(dtype == CCA_BF16, x, *w, y, false, RowDest{N, nullptr, 0, 1}, M, K, N, (hipStream_t)hip_stream) == hipSuccess
              ? CCA_OK
              : CCA_ERR_LAUNCH;
@@ -702,6 +704,8 @@ cca_status cca_decode_attention_mx(const cca_config *cfg, const cca_mx_cache *ca
     return CCA_ERR_ALIGN;
   if (!same_or_apart(weight_out, weight_in, (size_t)d.B * d.Hk * d.T * sizeof(float))) return CCA_ERR_UNSUPPORTED;
   if (!workspace || workspace_bytes < mx_attention_scratch_bytes(d)) return CCA_ERR_WORKSPACE;
+  const size_t q_bytes = (size_t)d.B * d.e_q * d.esize();
+  if (overlap(q, q_bytes, o, q_bytes)) return CCA_ERR_UNSUPPORTED;
   return mx_attention(d, *cache, q, false, len, max_len, 0, o, lse, weight_in, weight_out, workspace, (hipStream_t)hip_stream) == hipSuccess
              ? CCA_OK
              : CCA_ERR_LAUNCH;

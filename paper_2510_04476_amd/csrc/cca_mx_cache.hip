@@ -310,7 +310,7 @@ __global__ __launch_bounds__(SEL) void mx_select_kernel(EvictArgs a) {
       for (int e = 0; e < 4; ++e) k[e] = rank_key(wv[e], pv[e], old);
       return k;
     };
-    auto counts_of = [&](int row, mx_u4 k) __attribute__((always_inline)) {  // above | equal << 16: at most 8192 rows of a stretch to a lane
+    auto counts_of = [&](int row, mx_u4 k) __attribute__((always_inline)) {  // above | equal << 16
       int c = 0;
 #pragma unroll
       for (int e = 0; e < 4; ++e) c += row + e < n ? k[e] > prefix ? 1 : k[e] == prefix ? 1 << 16 : 0 : 0;

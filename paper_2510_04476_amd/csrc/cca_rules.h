@@ -484,7 +484,7 @@ inline MxSplit mx_split(long long groups, int T, int longest, int dh, bool joine
   const int round = dh <= 128 ? 256 : 128;  // rows of four wavefronts at a time
   if (!joined && longest <= (groups <= 256 ? 4 : 2) * round) return {1, longest > 0 ? longest : 1, groups <= 256 && longest > round};
   const int most = mx_max_splits(groups, T), even = (longest + most - 1) / most;
-    const int rows = (even > 0 ? (even + 127) / 128 : 1) * 128;  // (multiples of 64, 128 or 256: within 3 %)
+  const int rows = (even > 0 ? (even + 127) / 128 : 1) * 128;  // (multiples of 64, 128 or 256: within 3 %)
   return {longest > rows ? (longest + rows - 1) / rows : 1, rows, dh > 128};
 }
 

@@ -203,3 +203,44 @@ def test_config_reference_follows_its_fields_and_the_ring_depth_is_the_librarys(
             for k_ch in (1, 3):
                 cfg.flags, cfg.k_seq, cfg.k_ch = flags, k_seq, k_ch
                 assert cfg.ring_rows() == P.cca_decode_workspace_size(cfg)[1]
+
+
+def test_outputs_over_their_inputs_are_refused():
+    lib, cfg = P.load_library(), good()
+    cc, need, mc, w = cfg.c(), size(cfg)[1], cache(), B.cca_mx_weight(0x10000, 0x10000)
+    at = lambda a: C.c_void_p(0x100000 + a)
+    for dt, es in ((B.CCA_BF16, 2), (B.CCA_F32, 4)):
+        for y in (0, 3 * 64 * es - 16, -(3 * 5 * es) // 16 * 16 + 16):
+            assert lib.cca_project_mx(at(0), C.byref(w), at(y), 3, 64, 5, dt, None) == B.CCA_ERR_UNSUPPORTED
+    for o in (0, 2 * 256 * 2 - 16, 16 - 2 * 256 * 2):
+        assert lib.cca_decode_attention_mx(C.byref(cc), C.byref(mc), at(0), p, 8, at(o), None, None, None, p, need, None) == B.CCA_ERR_UNSUPPORTED
+
+
+def test_configs_caches_and_weights_can_be_copied_after_use_and_follow_their_storage():
+    import copy
+    import pickle
+    u8 = lambda *s: torch.zeros(*s, dtype=torch.uint8)
+    cfg = good()
+    cfg.ref()
+    for other in (copy.deepcopy(cfg), copy.copy(cfg), pickle.loads(pickle.dumps(cfg))):
+        assert other == cfg and other.ref() is not cfg.ref()
+        other.T = 96
+        assert cfg.ref()._obj.T == 64 and other.ref()._obj.T == 96
+    c = P.CCAMXCache(u8(2, 2, 64, 32), u8(2, 2, 2, 64), u8(2, 2, 64, 32), u8(2, 2, 2, 64), None, torch.zeros(2, 2, 64))
+    w = P.CCAMXWeight(u8(5, 32), u8(5, 2))
+    for make in (copy.deepcopy, lambda a: pickle.loads(pickle.dumps(a))):
+        c2, w2 = make(c), make(w)
+        assert c2._for(cfg)._obj.k_codes == c2.k_codes.data_ptr() != c.k_codes.data_ptr()
+        assert w2.ref()._obj.scales == w2.scales.data_ptr() != w.scales.data_ptr()
+    c.weight.data, w.codes.data = torch.ones(2, 2, 64), u8(5, 32)
+    assert c._for(cfg)._obj.weight == c.weight.data_ptr() and w.ref()._obj.codes == w.codes.data_ptr()
+    c.weight.data = torch.ones(2, 2, 32)
+    with pytest.raises(ValueError):
+        c._for(cfg)
+
+
+def test_loading_an_empty_prefill_enqueues_nothing():
+    cfg = good()
+    ring = torch.zeros(2, cfg.ring_rows(), cfg.n_lat, dtype=torch.bfloat16)
+    state = P.CCADecodeStateMX(P.CCAMXCache.allocate(cfg, "cpu"), ring, torch.zeros(0, dtype=torch.uint8))
+    state.load_prefill(cfg, None, 0)
