@@ -19,7 +19,7 @@ struct AttnArgs {
   const void *q;
   bool q_f32;  // q holds fp32 (of the storage type's values)
   const unsigned char *k_codes, *k_scales, *v_codes, *v_scales;
-  mx_f2 *state;   // (B, H_q, nsplit): m, l of a split (nsplit > 1)
+  mx_f2 *state;   // (B, H_q, nsplit): m, l of a split, where a second launch reads it, else null
   float *part;    // (B, H_q, nsplit, d_h): its o
   float *scores;  // (B, H_q, T) in log2 units, or null
   void *o;
@@ -342,9 +342,9 @@ __global__ __launch_bounds__(WAVES * 64, (WAVES == 4 ? Form<N32, TERMS>::RESIDEN
       acc = fmaf(src[4 + ch], f, acc);
     }
     const long long h = (long long)b * a.Hq + g * a.R + a.r0 + r;
-    if (a.state) {
-      const long long at = h * a.nsplit + split;
-      if (ch == 0) a.state[at] = mx_f2{M, L};
+    const long long at = h * a.nsplit + split;
+    if (a.state && ch == 0) a.state[at] = mx_f2{M, L};
+    if (a.nsplit > 1) {
       a.part[at * DH + ch] = acc;
     } else {
       const float res = L == 0.f ? 0.f : acc / L;
@@ -531,9 +531,8 @@ hipError_t mx_attention(const Dims &d, const cca_mx_cache &c, const void *q, boo
   const int longest = max_len + extra;
   const long long groups = (long long)d.B * d.Hk;
   // More heads to a group than one pass takes: their weights need a second launch, whatever the splits
-  const bool passes = d.R > 16;
-  const MxSplit split = mx_split(groups, d.T, longest, d.dh, weight_out && passes);
-  const bool finish = split.n > 1 || (weight_out && passes);
+  const MxSplit split = mx_split(groups, d.T, longest, d.dh);
+  const bool finish = split.n > 1 || (weight_out && d.R > 16);
   auto p = [](const void *x) { return static_cast<const unsigned char *>(x); };
   AttnArgs a{d.B, d.T, d.Hq, d.Hk, d.R, max_len, extra, split.n, split.rows, 0, d.scale * 1.44269504088896340736f, len, q, q_f32 || !d.bf16,
              p(c.k_codes), p(c.k_scales), p(c.v_codes), p(c.v_scales), finish ? reinterpret_cast<mx_f2 *>(ws + L.state) : nullptr,
@@ -549,7 +548,8 @@ hipError_t mx_attention(const Dims &d, const cca_mx_cache &c, const void *q, boo
   if (!finish) return hipSuccess;
   const int tiles = weight_out ? (longest + W_ROWS - 1) / W_ROWS : 0;
   const int ch = split.n <= 64 ? 64 : 16;
-  const long long joins = (long long)d.B * d.Hq * ((d.dh + ch - 1) / ch), items = joins + groups * tiles;
+  const long long joins = split.n > 1 ? (long long)d.B * d.Hq * ((d.dh + ch - 1) / ch) : 0, items = joins + groups * tiles;
+  if (items == 0) return hipSuccess;
   const unsigned grid = (unsigned)(items < (1 << 20) ? items : 1 << 20);
   if (d.bf16 && ch == 64) mx_finish_kernel<bf16_t, 64><<<grid, 256, 0, s>>>(a, d.dh, joins, tiles);
   else if (d.bf16) mx_finish_kernel<bf16_t, 16><<<grid, 256, 0, s>>>(a, d.dh, joins, tiles);

@@ -468,8 +468,9 @@ constexpr size_t DECODE_UP_LDS = decode_up_lds(1, UP_CHANNELS);
 // rows, heads): 32 x 16384, 8 / 2 x 128: 29.2, 30.2, 31.9, 31.0; 16 x 16384: 17.6, 19.2; 48 x 8000, 4 / 1: 16.3, 18.0; 100 x 2000: 13.5,
 // 20.9; 20 x 3000, 4 / 4 x 256: 21.3, 20.3, of eight wavefronts 20.2; 7 x 9000: 19.3, 19.0, 18.9; 13 x 5003 of mixed lengths, 16 / 4 x 64, half of its workgroups
 // without rows: 11.5, 11.8, 10.6, 10.7.
-// `joined`: a second launch is needed anyway.  Else a head of few rounds goes to one workgroup - of eight wavefronts where that leaves CUs idle -
-// and the second launch is saved: 1 x 1000: 7.8 us either way, a launch less for the host; 48 x 300, 8 x 32: 5.5, split 9.2.
+// A head of few rounds goes to one workgroup - of eight wavefronts where that leaves CUs idle - which writes the result and adds up the
+// weights itself.  Without weights 1 x 1000: 7.8 us either way, a launch less for the host; 48 x 300, 8 x 32: 5.5, split 9.2.  With them, of
+// 6 sequences, 8 / 2 x 128: 500 rows 6.8, split 8.1; 1000 rows 9.1, 8.2; 16 / 1 x 64, 1000 rows 10.3, 12.3.
 struct MxSplit {
   int n, rows;  // splits, rows of each
   bool many;    // 8 wavefronts to a workgroup, else 4
@@ -480,9 +481,9 @@ inline int mx_max_splits(long long groups, int T) {
   const long long s = want < rounds ? want : rounds;
   return (int)(s < MX_MAX_SPLITS ? s : MX_MAX_SPLITS);
 }
-inline MxSplit mx_split(long long groups, int T, int longest, int dh, bool joined) {
+inline MxSplit mx_split(long long groups, int T, int longest, int dh) {
   const int round = dh <= 128 ? 256 : 128;  // rows of four wavefronts at a time
-  if (!joined && longest <= (groups <= 256 ? 4 : 2) * round) return {1, longest > 0 ? longest : 1, groups <= 256 && longest > round};
+  if (longest <= (groups <= 256 ? 4 : 2) * round) return {1, longest > 0 ? longest : 1, groups <= 256 && longest > round};
   const int most = mx_max_splits(groups, T), even = (longest + most - 1) / most;
   const int rows = (even > 0 ? (even + 127) / 128 : 1) * 128;  // (multiples of 64, 128 or 256: within 3 %)
   return {longest > rows ? (longest + rows - 1) / rows : 1, rows, dh > 128};

@@ -116,6 +116,23 @@ def test_attention(i):
     check_attention(cfg, vals, q, lens, o3, lse3, w, None, before)
 
 
+@pytest.mark.parametrize("Bn,T,Hq,Hk,dh,dt", [(3, 320, 20, 1, 64, "bf16"), (130, 96, 36, 2, 32, "bf16"), (2, 64, 17, 1, 128, "f32"), (2, 4096, 24, 1, 64, "bf16")])
+def test_attention_with_more_heads_than_a_pass_takes(Bn, T, Hq, Hk, dh, dt):
+    """One workgroup to a head of the cache or several, in passes over the query heads; the weights are added up over all of them."""
+    say("case passes", Bn, T, Hq, Hk, dh, dt)
+    cfg = config(Bn, T, Hq, Hk, dh, dt)
+    lens = np.random.default_rng(T).integers(0, T + 1, Bn)
+    lens[0], lens[-1] = 0, T
+    cache, vals = random_cache(cfg, 7, lens)
+    q = rounded(np.random.default_rng(8).standard_normal((Bn, Hq, dh)), dt).cuda()
+    before = cache.weight.clone()
+    o, lse = P.cca_decode_attention_mx(cfg, cache, q, i32(lens), T, want_lse=True, weight_in=before, weight_out=cache.weight)
+    torch.cuda.synchronize()
+    check_attention(cfg, vals, q, lens, o, lse, cache.weight, before, before)
+    o, lse = P.cca_decode_attention_mx(cfg, cache, q, i32([0] * Bn), 0, want_lse=True, weight_in=before, weight_out=cache.weight.copy_(before))
+    assert (o == 0).all() and torch.isneginf(lse).all() and torch.equal(cache.weight, before)
+
+
 def test_attention_contents():
     """NaN and infinite queries, a NaN group among the rows (its sequence and head alone are NaN), scores far apart, lengths out of range
     (clamped), weights in place."""

@@ -187,10 +187,9 @@ def test_splits_fit_the_workspace_and_whole_rounds(groups):
     for T in (32, 64, 320, 1024, 8192, 100000, 1 << 22):
         for dh in (32, 64, 96, 128, 160, 256):
             for longest in {1, 2, T // 3 + 1, T - 1, T}:
-                for weights in (False, True):
-                    n, rows, _ = rules_mx.split(groups, T, longest, dh, weights)
-                    assert 1 <= n <= rules_mx.max_splits(groups, T) <= 256 and rows > 0
-                    assert -(-longest // rows) == n and (n == 1 or rows % (64 if dh <= 128 else 32) == 0)
+                n, rows, _ = rules_mx.split(groups, T, longest, dh)
+                assert 1 <= n <= rules_mx.max_splits(groups, T) <= 256 and rows > 0
+                assert -(-longest // rows) == n and (n == 1 or rows % (64 if dh <= 128 else 32) == 0)
 
 
 def test_config_reference_follows_its_fields_and_the_ring_depth_is_the_librarys():
