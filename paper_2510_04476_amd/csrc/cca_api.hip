@@ -595,7 +595,7 @@ static cca_status mx_dims(const cca_config *cfg, Dims *d) {
   cca_status st = make_dims(cfg, d);
   if (st != CCA_OK) return st;
   if (d->dh % 32 != 0 || d->T % 32 != 0) return CCA_ERR_UNSUPPORTED;
-  if ((long long)d->B * d->Hk > (1ll << 22)) return CCA_ERR_SHAPE;  // workgroups of a launch
+  if ((long long)d->B * d->Hk * ((d->R + 15) / 16) > (1ll << 22)) return CCA_ERR_SHAPE;  // workgroups of a launch
   return CCA_OK;
 }
 static bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
@@ -739,6 +739,7 @@ cca_status cca_decode_step_mx(const cca_config *cfg, const cca_weights *w, const
   cca_status st = mx_dims(cfg, &d);
   if (st != CCA_OK) return st;
   if (d.E % 32 != 0) return CCA_ERR_UNSUPPORTED;
+  if (d.B > 65536) return CCA_ERR_SHAPE;  // rows of a projection
   if (!w || !x_new || !lat_ring || !pos || !len || !out) return CCA_ERR_NULL;
   if ((st = mx_weight_check(w_down)) != CCA_OK || (st = mx_weight_check(w_out)) != CCA_OK) return st;
   if ((st = mx_cache_check(cache)) != CCA_OK) return st;

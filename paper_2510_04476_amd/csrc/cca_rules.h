@@ -462,7 +462,7 @@ constexpr size_t decode_up_lds(long long B, int e_q) { return (size_t)((e_q + 12
 constexpr size_t DECODE_UP_LDS = decode_up_lds(1, UP_CHANNELS);
 
 // ---- attention over the 4-bit cache: rows of a split ----------------------------------------------------------------------
-// groups = sequences x KV heads.  A wavefront asks for a block of 64 rows (32 above d_h = 128, both 8.5 KB at the usual widths) ahead of
+// groups = sequences x KV heads (x passes over more than 16 query heads).  A wavefront asks for a block of 64 rows (32 above d_h = 128, both 8.5 KB at the usual widths) ahead of
 // the one that it multiplies, and one wavefront to a SIMD already keeps the memory busy: splits that make about one workgroup of four to
 // a CU (of eight wavefronts above d_h = 128), so that each streams for long.  Call with its second launch, 256, 512, 768, 1024 workgroups, us (sequences x
 // rows, heads): 32 x 16384, 8 / 2 x 128: 29.2, 30.2, 31.9, 31.0; 16 x 16384: 17.6, 19.2; 48 x 8000, 4 / 1: 16.3, 18.0; 100 x 2000: 13.5,

@@ -243,3 +243,16 @@ def test_loading_an_empty_prefill_enqueues_nothing():
     ring = torch.zeros(2, cfg.ring_rows(), cfg.n_lat, dtype=torch.bfloat16)
     state = P.CCADecodeStateMX(P.CCAMXCache.allocate(cfg, "cpu"), ring, torch.zeros(0, dtype=torch.uint8))
     state.load_prefill(cfg, None, 0)
+
+
+def test_batches_beyond_a_launch_are_refused():
+    cfg = P.CCAConfig(B=1 << 21, T=32, d_model=2048, n_q_heads=32, n_kv_heads=1, head_dim=64)  # two passes of 16 heads each
+    assert size(cfg)[0] == B.CCA_OK
+    cfg.B += 1
+    assert size(cfg)[0] == B.CCA_ERR_SHAPE
+    cfg = P.CCAConfig(B=65537, T=32, d_model=256, n_q_heads=4, n_kv_heads=2, head_dim=64)
+    w, mw = B.cca_weights(None, p, p, p, None, None), B.cca_mx_weight(0x10000, 0x10000)
+    step = lambda: P.load_library().cca_decode_step_mx(C.byref(cfg.c()), C.byref(w), C.byref(mw), C.byref(mw), p, C.byref(cache()), p, p, p, 31, p, p, 8, None)
+    assert step() == B.CCA_ERR_SHAPE
+    cfg.B = 65536
+    assert step() == B.CCA_ERR_WORKSPACE
