@@ -398,7 +398,7 @@ __device__ __forceinline__ mx_f2 joined(const mx_f2 *state, int n, int lane, mx_
   float M = -INFINITY;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    st[i] = state[min(64 * i + lane, n - 1)];
+    st[i] = state[(uint32_t)min(64 * i + lane, n - 1)];
     if (64 * i + lane >= n) st[i] = mx_f2{-INFINITY, 0.f};
     M = fmaxf(M, st[i][0]);
   }
@@ -410,21 +410,22 @@ __device__ __forceinline__ mx_f2 joined(const mx_f2 *state, int n, int lane, mx_
 }
 // CH: channels of a workgroup that joins; 256 / CH parts of it share the splits, 16 each, so that all are requested at once.
 template <typename T, int CH>
-__global__ __launch_bounds__(256) void mx_finish_kernel(AttnArgs a, int dh, long long joins, int tiles) {
+__global__ __launch_bounds__(256) void mx_finish_kernel(AttnArgs a, int dh, unsigned joins, unsigned items, int tiles) {
   constexpr int PARTS = 256 / CH;
   __shared__ float f[256], acc[PARTS][CH], top[W_HEADS], inv[W_HEADS];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  for (long long item = blockIdx.x; item < joins + (long long)a.B * a.Hk * tiles; item += gridDim.x, __syncthreads()) {
+  for (unsigned item = blockIdx.x; item < items; item += gridDim.x, __syncthreads()) {
     mx_f2 st[4];
     if (item < joins) {
-      const int chunks = (dh + CH - 1) / CH, part = tid / CH, ch = (int)(item % chunks) * CH + tid % CH;
+      const unsigned chunks = (unsigned)(dh + CH - 1) / CH;
+      const int part = tid / CH, ch = (int)(item % chunks) * CH + tid % CH;
       const long long bh = item / chunks;
       // requested before anything is known of the sequence's length (a place that no split wrote is read, never used)
-      const float *src = a.part + bh * a.nsplit * dh + min(ch, dh - 1);
+      const float *src = a.part + bh * a.nsplit * dh;
       float v[16];
 #pragma unroll
-      for (int u = 0; u < 16; ++u) v[u] = src[(long long)min(part + PARTS * u, a.nsplit - 1) * dh];
-      const int len = seq_len(a, (int)(bh / a.Hq)), n = max(1, min(a.nsplit, (len + a.per - 1) / a.per));
+      for (int u = 0; u < 16; ++u) v[u] = src[(uint32_t)(min(part + PARTS * u, a.nsplit - 1) * dh + min(ch, dh - 1))];
+      const int len = seq_len(a, (int)(item / chunks / (unsigned)a.Hq)), n = max(1, min(a.nsplit, (len + a.per - 1) / a.per));
       const mx_f2 ml = joined(a.state + bh * a.nsplit, n, lane, st);  // every wavefront for itself
       const mx_f2 mine = wave == 0 ? st[0] : wave == 1 ? st[1] : wave == 2 ? st[2] : st[3];
       f[tid] = rescale(mine[0], mine[1], ml[0]);  // of split `tid`
@@ -443,29 +444,33 @@ __global__ __launch_bounds__(256) void mx_finish_kernel(AttnArgs a, int dh, long
       }
       continue;
     }
-    const long long head = (item - joins) / tiles;
-    const int b = (int)(head / a.Hk), g = (int)(head % a.Hk), len = seq_len(a, b), row0 = (int)((item - joins) % tiles) * W_ROWS;
+    const unsigned tile = item - joins, bg = tile / (unsigned)tiles;
+    const long long head = bg;
+    const int b = (int)(bg / (unsigned)a.Hk), g = (int)(bg % (unsigned)a.Hk), len = seq_len(a, b), row0 = (int)(tile % (unsigned)tiles) * W_ROWS;
     if (row0 >= len) continue;
     const int n = min(a.nsplit, (len + a.per - 1) / a.per), old = len - a.extra;  // the new rows of a step start from 0
     const int row = row0 + 4 * tid, at = min(row, a.T - 4);  // rows past the capacity are read at its end, never stored
     mx_f4 sum = {0.f, 0.f, 0.f, 0.f}, before = sum;
     if (a.weight_in) before = *reinterpret_cast<const mx_f4 *>(a.weight_in + head * a.T + at);
+#pragma unroll 1
     for (int r0 = 0; r0 < a.R; r0 += W_HEADS) {
       const int nr = min(W_HEADS, a.R - r0);
       const long long h0 = (long long)b * a.Hq + g * a.R + r0;
-      const float *const sc = a.scores + h0 * a.T + at;
+      const float *const sc = a.scores + h0 * a.T;
       mx_f4 s[4];
       auto request = [&](int r) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) s[u] = *reinterpret_cast<const mx_f4 *>(sc + (long long)min(r + u, nr - 1) * a.T);
+        for (int u = 0; u < 4; ++u) s[u] = *reinterpret_cast<const mx_f4 *>(sc + (long long)min(r + u, nr - 1) * a.T + (uint32_t)at);
       };
       request(0);  // with the states: one latency for both
       if (r0) __syncthreads();
+#pragma unroll 1
       for (int r = wave; r < nr; r += 4) {
         const mx_f2 ml = joined(a.state + (h0 + r) * a.nsplit, n, lane, st);
         if (lane == 0) top[r] = ml[0] == -INFINITY ? 0.f : ml[0], inv[r] = ml[1] == 0.f ? 0.f : 1.f / ml[1];
       }
       __syncthreads();
+#pragma unroll 1
       for (int r = 0; r < nr; r += 4) {
         if (r) request(r);
 #pragma unroll
@@ -546,13 +551,14 @@ hipError_t mx_attention(const Dims &d, const cca_mx_cache &c, const void *q, boo
   if (e != hipSuccess || !finish) return e;
   const int tiles = weight_out ? (longest + W_ROWS - 1) / W_ROWS : 0;
   const int ch = split.n <= 64 ? 64 : 16;
+  // (32 bits hold them: with a second launch the workspace holds 4 bytes to a score, 4 d_h to a split)
   const long long joins = split.n > 1 ? (long long)d.B * d.Hq * ((d.dh + ch - 1) / ch) : 0, items = joins + groups * tiles;
   if (items == 0) return hipSuccess;
   const unsigned grid = (unsigned)(items < (1 << 20) ? items : 1 << 20);
-  if (d.bf16 && ch == 64) mx_finish_kernel<bf16_t, 64><<<grid, 256, 0, s>>>(a, d.dh, joins, tiles);
-  else if (d.bf16) mx_finish_kernel<bf16_t, 16><<<grid, 256, 0, s>>>(a, d.dh, joins, tiles);
-  else if (ch == 64) mx_finish_kernel<float, 64><<<grid, 256, 0, s>>>(a, d.dh, joins, tiles);
-  else mx_finish_kernel<float, 16><<<grid, 256, 0, s>>>(a, d.dh, joins, tiles);
+  if (d.bf16 && ch == 64) mx_finish_kernel<bf16_t, 64><<<grid, 256, 0, s>>>(a, d.dh, (unsigned)joins, (unsigned)items, tiles);
+  else if (d.bf16) mx_finish_kernel<bf16_t, 16><<<grid, 256, 0, s>>>(a, d.dh, (unsigned)joins, (unsigned)items, tiles);
+  else if (ch == 64) mx_finish_kernel<float, 64><<<grid, 256, 0, s>>>(a, d.dh, (unsigned)joins, (unsigned)items, tiles);
+  else mx_finish_kernel<float, 16><<<grid, 256, 0, s>>>(a, d.dh, (unsigned)joins, (unsigned)items, tiles);
   return hipGetLastError();
 }
 
