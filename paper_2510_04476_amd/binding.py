@@ -525,6 +525,12 @@ def _mx_ptr(name, t, shape, dtype, index):
     return t.data_ptr()
 
 
+def _mx_workspace(t, index):
+    if t.dtype is not torch.uint8 or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"workspace: {t.dtype} on {t.device}, expected contiguous torch.uint8 on {'the CPU' if index < 0 else f'GPU {index}'}")
+    return t.data_ptr()
+
+
 def _mx_opt(name, t, shape, dtype, index):
     return None if t is None else _mx_ptr(name, t, shape, dtype, index)
 
@@ -562,7 +568,8 @@ class CCAMXWeight:
             raise ValueError(f"codes: {tuple(self.codes.shape)}, expected (N, K/2)")
         n, k, index = self.codes.shape[0], 2 * self.codes.shape[1], self.codes.get_device()
         c = cca_mx_weight(_mx_ptr("codes", self.codes, (n, k // 2), torch.uint8, index), _mx_ptr("scales", self.scales, (n, k // 32), torch.uint8, index))
-        for name, v in (("K", k), ("N", n), ("_index", index), ("_at", (c.codes, c.scales)), ("_c", c), ("_kept", C.byref(c))):
+        for name, v in (("K", k), ("N", n), ("_index", index), ("_now", (self.codes.data_ptr, self.scales.data_ptr)), ("_key", (c.codes, c.scales)), ("_c", c),
+                        ("_kept", C.byref(c))):
             object.__setattr__(self, name, v)
 
     def __reduce__(self):
@@ -570,7 +577,8 @@ class CCAMXWeight:
 
     def ref(self):
         """The C form by reference, made again where a tensor has got another storage."""
-        if (self.codes.data_ptr(), self.scales.data_ptr()) != self._at:
+        a, b = self._now
+        if (a(), b()) != self._key:
             self.__post_init__()
         return self._kept
 
@@ -596,17 +604,14 @@ class CCAMXCache:
                                 ("pos", (B, Hk, T), torch.int32), ("weight", (B, Hk, T), torch.float32)):
             ptrs[name] = _mx_opt(name, getattr(self, name), shape, dt, index)
         c = cca_mx_cache(**ptrs)
-        for name, v in (("_index", index), ("_device", self.k_codes.device), ("_layout", (B, Hk, T, 2 * half)), ("_at", self._now()), ("_c", c),
-                        ("_kept", C.byref(c))):
+        order = tuple(ptrs)
+        now = tuple(type(None) if getattr(self, name) is None else getattr(self, name).data_ptr for name in order)  # (called: the address, or None)
+        for name, v in (("_index", index), ("_device", self.k_codes.device), ("_layout", (B, Hk, T, 2 * half)), ("_now", now), ("_c", c),
+                        ("_key", (*(ptrs[name] for name in order), B, Hk, T, 2 * half)), ("_kept", C.byref(c))):
             object.__setattr__(self, name, v)
 
     def __reduce__(self):
         return CCAMXCache, (self.k_codes, self.k_scales, self.v_codes, self.v_scales, self.pos, self.weight)
-
-    def _now(self):
-        pos, weight = self.pos, self.weight
-        return (self.k_codes.data_ptr(), self.k_scales.data_ptr(), self.v_codes.data_ptr(), self.v_scales.data_ptr(),
-                None if pos is None else pos.data_ptr(), None if weight is None else weight.data_ptr())
 
     @staticmethod
     def allocate(cfg: CCAConfig, device, with_weights: bool = True) -> "CCAMXCache":
@@ -617,11 +622,11 @@ class CCAMXCache:
                           z(B, Hk, T, dtype=torch.float32) if with_weights else None)
 
     def _for(self, cfg: CCAConfig):
-        if self._layout != (cfg.B, cfg.n_kv_heads, cfg.T, cfg.head_dim):
-            raise ValueError(f"cache of (B, H_k, T, d_h) = {self._layout}, config of {(cfg.B, cfg.n_kv_heads, cfg.T, cfg.head_dim)}")
-        if self._now() != self._at:  # a tensor has got another storage
-            self.__post_init__()
-            return self._for(cfg)
+        a, b, c, d, e, f = self._now
+        if (a(), b(), c(), d(), e(), f(), cfg.B, cfg.n_kv_heads, cfg.T, cfg.head_dim) != self._key:
+            self.__post_init__()  # a tensor may have got another storage
+            if self._layout != (cfg.B, cfg.n_kv_heads, cfg.T, cfg.head_dim):
+                raise ValueError(f"cache of (B, H_k, T, d_h) = {self._layout}, config of {(cfg.B, cfg.n_kv_heads, cfg.T, cfg.head_dim)}")
         return self._kept
 
 
@@ -696,7 +701,7 @@ def cca_decode_attention_mx(cfg: CCAConfig, cache: CCAMXCache, q, lens, max_len:
     _mx_call("cca_decode_attention_mx", index, cfg.ref(), cache._for(cfg), _mx_ptr("q", q, (B, Hq, dh), dt, index),
              _mx_ptr("lens", lens, (B,), torch.int32, index), max_len, o_ptr, lse_ptr, _mx_opt("weight_in", weight_in, w, torch.float32, index),
              _mx_opt("weight_out", weight_out, w, torch.float32, index),
-             _mx_ptr("workspace", workspace, workspace.shape, torch.uint8, index), workspace.numel())
+             _mx_workspace(workspace, index), workspace.numel())
     return (o, lse) if want_lse else o
 
 
@@ -711,7 +716,7 @@ def cca_cache_evict_mx(cfg: CCAConfig, cache: CCAMXCache, lens, max_len: int, bu
     _mx_call("cca_cache_evict_mx", index, cfg.ref(), cache._for(cfg), _mx_ptr("lens", lens, (cfg.B,), torch.int32, index), max_len, budget,
              recent, _mx_opt("weight_out", weight_out, w, torch.float32, index), _mx_opt("pos_out", pos_out, w, torch.int32, index),
              _mx_opt("lens_out", lens_out, (cfg.B,), torch.int32, index),
-             _mx_ptr("workspace", workspace, workspace.shape, torch.uint8, index), workspace.numel())
+             _mx_workspace(workspace, index), workspace.numel())
 
 
 @dataclass
@@ -752,7 +757,7 @@ def cca_decode_step_mx(cfg: CCAConfig, w: CCAWeights, w_down: CCAMXWeight, w_out
     _mx_call("cca_decode_step_mx", index, cfg.ref(), C.byref(cw), w_down.ref(), w_out.ref(), _mx_ptr("x_new", x_new, x_shape, dt, index),
              state.cache._for(cfg), _mx_ptr("lat_ring", state.lat_ring, ring, dt, index), _mx_ptr("pos", pos, per_seq, torch.int32, index),
              _mx_ptr("lens", lens, per_seq, torch.int32, index), max_len, out_ptr,
-             _mx_ptr("workspace", ws, ws.shape, torch.uint8, index), ws.numel())
+             _mx_workspace(ws, index), ws.numel())
     return out
 
 
