@@ -25,6 +25,8 @@ struct ProjArgs {
 // read by lanes from memory, every lane's 16 bytes lie in a line of their own, which took 38 us for 32 x 8192 x 8192.  16-byte chunk c of
 // row r lies at place c ^ r (fp32: pairs of chunks), so that 16 rows of one chunk fall into different banks.
 // fp32: x in three parts of bf16, three products.
+// Bound by what a CU takes in, about 20 bytes a ns of W from memory and 54 of x from the L2, and below that by one latency: 1 x 2048 x 1536 3.5 us;
+// 32 x 8192 x 8192 14.1 us, 2.5 TB/s of W beside 512 KB of x to a CU.
 // ---------------------------------------------------------------------------
 template <typename T, int ROWS, int CT>
 struct ProjForm {
@@ -179,7 +181,8 @@ __global__ __launch_bounds__(WAVES * 64) void mx_project_kernel(ProjArgs a) {
   }
 }
 
-// W (K, N) -> codes, scales: a thread per (column, group), columns along the threads
+// W (K, N) -> codes, scales: a thread per (column, group), columns along the threads.  Once for a set of weights; bound by reading W: 8192 x
+// 8192 bf16 47 us, 3.6 TB/s, fp32 67 us, 4.5.
 template <typename T>
 __global__ __launch_bounds__(256) void mx_quantize_kernel(const T *__restrict__ w, int K, int N, unsigned char *__restrict__ codes,
                                                          unsigned char *__restrict__ scales) {
