@@ -158,8 +158,8 @@ __global__ __launch_bounds__(256) void mx_rows_kernel(StoreArgs a, T *__restrict
 // those that equal it the first.  Then each wavefront counts both kinds in its own stretch of rows and, behind one sum over the
 // wavefronts, numbers the holes below `budget` and the kept rows beyond it.
 // HELD: the keys lie in LDS, so that weights and positions are read once; longer heads are read again by every pass.
-// Bound by one workgroup's chain - three digits with three barriers each, two passes before and two behind - and, on long heads, by what one CU
-// takes in: 256 rows 8.7 us, 1024 10.4, 4608 12.4, 16000 18.2, 30011 24.8, 60000 (read again) 63.
+// Bound by one workgroup's chain - three digits with three barriers each, a pass before and two behind - and, on long heads, by its vector
+// instructions: 256 rows 8.8 us, 1024 9.1, 4608 12.5, 16000 16.3, 32000 21.8, 60000 (read again) 52.7.
 // ---------------------------------------------------------------------------
 constexpr int SEL = 1024, DIGIT = 11, COPIES = 2;
 constexpr int HELD_ROWS = 32768;  // 128 KB of keys beside 16 KB of histogram
@@ -176,9 +176,10 @@ struct EvictArgs {
 };
 typedef int mx_i4 __attribute__((ext_vector_type(4)));
 
-__device__ __forceinline__ uint32_t rank_key(float w, int pos, long long old) {
-  const uint32_t u = __float_as_uint(w + 0.f), k = (u & 0x80000000u) ? ~u : u | 0x80000000u;  // -0 counts as 0
-  return (long long)pos > old ? 0xffffffffu : w != w ? 0u : k;
+// (no position exceeds the newest one: their difference fits 32 bits)
+__device__ __forceinline__ uint32_t rank_key(float w, int pos, int newest, int recent) {
+  const uint32_t u = __float_as_uint(w + 0.f), k = u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);  // -0 counts as 0
+  return (uint32_t)newest - (uint32_t)pos < (uint32_t)recent ? 0xffffffffu : w != w ? 0u : k;
 }
 // Sum over the lanes up to this one: shifts inside each row of 16 lanes, then the rows' last sums handed on
 __device__ __forceinline__ int wave_scan(int x) {
@@ -195,7 +196,7 @@ __global__ __launch_bounds__(SEL) void mx_select_kernel(EvictArgs a) {
   extern __shared__ __attribute__((aligned(16))) int sel_lds[];
   int *const hist = sel_lds;                                                        // [bin][copy]
   uint32_t *const keys = reinterpret_cast<uint32_t *>(sel_lds + (COPIES << DIGIT));  // HELD: of every row
-  __shared__ int red[SEL / 64][2], found[2];
+  __shared__ int red[SEL / 64][2], found[3];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   for (long long head = blockIdx.x; head < a.heads; head += gridDim.x, __syncthreads()) {
     const float *const w = a.weight + head * a.T;
@@ -211,35 +212,29 @@ __global__ __launch_bounds__(SEL) void mx_select_kernel(EvictArgs a) {
         for (int i = tid; i < n; i += SEL) wo[i] = w[i], po[i] = p[i];
       continue;
     }
-    // Rows four at a time, four groups requested together; the capacity is a multiple of 32, so a group that begins below n is inside it.
-    // (Loops stay rolled: a launch runs them a few times, and code that it has to fetch first costs more than the iterations.  With the
-    // rows of 8 iterations unrolled into registers: 4608 and 30011 rows 17.6 and 38.6 us.)
-    auto groups = [&](auto f) __attribute__((always_inline)) {
-#pragma unroll 1
-      for (int r0 = 4 * tid; r0 < n; r0 += 16 * SEL) {
-        mx_f4 wv[4];
-        mx_i4 pv[4];
+    // Rows four at a time, several groups requested together; the capacity is a multiple of 32, so a group that begins below n is inside it.
+    // Lanes past the end repeat the last group.  (Loops stay rolled: a launch runs them a few times, and code that it has to fetch first
+    // costs more than the iterations.  With the rows of 8 iterations unrolled into registers: 4608 and 30011 rows 17.6 and 38.6 us.)
+    const int last = (n - 1) & ~3;
+    auto request = [&](const auto *from, int r0, auto (&to)[4]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const int at = min(r0 + 4 * SEL * u, a.T - 4);
-          wv[u] = *reinterpret_cast<const mx_f4 *>(w + at);
-          pv[u] = *reinterpret_cast<const mx_i4 *>(p + at);
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-          if (r0 + 4 * SEL * u < n) f(r0 + 4 * SEL * u, wv[u], pv[u]);
-      }
+      for (int u = 0; u < 4; ++u) to[u] = *reinterpret_cast<const std::remove_reference_t<decltype(to[0])> *>(from + min(r0 + 4 * SEL * u, last));
     };
+    mx_f4 wv[4];
+    if constexpr (HELD) request(w, 4 * tid, wv);  // the first weights beside the positions, which wait in LDS
     int newest = INT32_MIN;
 #pragma unroll 1
     for (int r0 = 4 * tid; r0 < n; r0 += 32 * SEL) {
       mx_i4 pv[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) pv[u] = *reinterpret_cast<const mx_i4 *>(p + min(r0 + 4 * SEL * u, a.T - 4));
+      for (int u = 0; u < 8; ++u) pv[u] = *reinterpret_cast<const mx_i4 *>(p + min(r0 + 4 * SEL * u, last));
 #pragma unroll
-      for (int u = 0; u < 8; ++u)
+      for (int u = 0; u < 8; ++u) {
+        const int row = r0 + 4 * SEL * u;
+        if (HELD && row < n) *reinterpret_cast<mx_i4 *>(keys + row) = pv[u];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) newest = r0 + 4 * SEL * u + e < n ? max(newest, pv[u][e]) : newest;
+        for (int e = 0; e < 4; ++e) newest = row + e < n ? max(newest, pv[u][e]) : newest;
+      }
     }
     for (int off = 32; off > 0; off >>= 1) newest = max(newest, __shfl_xor(newest, off));
     if (lane == 0) red[wave][0] = newest;
@@ -247,34 +242,58 @@ __global__ __launch_bounds__(SEL) void mx_select_kernel(EvictArgs a) {
     __syncthreads();
 #pragma unroll
     for (int x = 0; x < SEL / 64; ++x) newest = max(newest, red[x][0]);
-    const long long old = (long long)newest - a.recent;  // the largest position that is not recent
+    // keys of rows `row` ... `row` + 3; those from n on have the lowest, and are the last of it: they never stay
+    auto keys_of = [&](int row, mx_f4 wv, mx_i4 pv) __attribute__((always_inline)) {
+      mx_u4 k;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) k[e] = rank_key(wv[e], pv[e], newest, a.recent);
+      if (row + 4 > n) {
+#pragma unroll
+        for (int e = 1; e < 4; ++e) k[e] = row + e < n ? k[e] : 0u;
+      }
+      return k;
+    };
     uint32_t prefix = 0, mask = 0;
     int want = a.budget;  // how many of the rows that agree with the prefix are still to be taken
 #pragma unroll 1
     for (int pass = 0; pass < 3; ++pass) {
       const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
       const uint32_t bins = pass == 2 ? 1023u : 2047u;
-      auto count = [&](int row, uint32_t k) __attribute__((always_inline)) {
-        if (row < n && (k & mask) == prefix) atomicAdd(&hist[((k >> shift) & bins) * COPIES + (lane & (COPIES - 1))], 1);
+      auto count = [&](uint32_t k) __attribute__((always_inline)) {
+        if ((k & mask) == prefix) atomicAdd(&hist[((k >> shift) & bins) * COPIES + (lane & (COPIES - 1))], 1);
       };
       if (HELD && pass > 0) {
 #pragma unroll 1
         for (int r = 4 * tid; r < n; r += 4 * SEL) {
           const mx_u4 k = *reinterpret_cast<const mx_u4 *>(keys + r);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) count(r + e, k[e]);
+          for (int e = 0; e < 4; ++e) count(k[e]);
         }
       } else {
-        groups([&](int row, mx_f4 wv, mx_i4 pv) __attribute__((always_inline)) {
-          mx_u4 k;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t ke = rank_key(wv[e], pv[e], old);
-            k[e] = ke;
-            count(row + e, ke);
+#pragma unroll 1
+        for (int r0 = 4 * tid; r0 < n; r0 += 16 * SEL) {
+          mx_f4 next[4];
+          mx_i4 pv[4];
+          if constexpr (HELD) {
+            request(w, r0 + 16 * SEL, next);
+          } else {
+            request(w, r0, wv);
+            request(p, r0, pv);
           }
-          if constexpr (HELD) *reinterpret_cast<mx_u4 *>(keys + row) = k;
-        });
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int row = r0 + 4 * SEL * u;
+            if (row >= n) continue;
+            if constexpr (HELD) pv[u] = *reinterpret_cast<const mx_i4 *>(keys + row);
+            const mx_u4 k = keys_of(row, wv[u], pv[u]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) count(k[e]);
+            if constexpr (HELD) *reinterpret_cast<mx_u4 *>(keys + row) = k;
+          }
+          if constexpr (HELD)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) wv[u] = next[u];
+        }
       }
       __syncthreads();
       // from the top: thread t holds two neighbouring bins, which it clears; the first bin at which the sum reaches `want`
@@ -293,74 +312,97 @@ __global__ __launch_bounds__(SEL) void mx_select_kernel(EvictArgs a) {
       int before = sum - c[0] - c[1];
 #pragma unroll
       for (int x = 0; x < SEL / 64; ++x) before += x < wave ? red[x][1] : 0;
-      if (before < want && before + c[0] >= want) found[0] = hi, found[1] = before;
-      else if (before + c[0] < want && before + c[0] + c[1] >= want) found[0] = hi - 1, found[1] = before + c[0];
+      if (before < want && before + c[0] >= want) found[0] = hi, found[1] = before, found[2] = c[0];
+      else if (before + c[0] < want && before + c[0] + c[1] >= want) found[0] = hi - 1, found[1] = before + c[0], found[2] = c[1];
       __syncthreads();
       prefix |= (uint32_t)found[0] << shift;
       mask |= bins << shift;
       want -= found[1];
       // (`found` and `red` are written again behind the next pass's barriers)
     }
-    // `want` rows of key `prefix` stay, the first ones.  A wavefront's stretch: whole lines of 256 rows
+    // Rows above `thr` stay.  With more rows of key `prefix` than `want`, of those the first; else they count as above.  (All n > budget rows
+    // cannot be above: without ties prefix > 0.)
+    const bool ties = found[2] > want;
+    const uint32_t thr = ties ? prefix : prefix - 1;
+    // A wavefront's stretch: whole lines of 256 rows
     const int stretch = ((n + SEL / 64 - 1) / (SEL / 64) + 255) / 256 * 256, r0 = wave * stretch, r1 = min(n, r0 + stretch);
-    // keys of rows `row` ... `row` + 3, this lane's (row is below n)
     auto keys_at = [&](int row) __attribute__((always_inline)) {
+      if (row >= n) return mx_u4{0u, 0u, 0u, 0u};
       if constexpr (HELD) return *reinterpret_cast<const mx_u4 *>(keys + row);
-      const mx_f4 wv = *reinterpret_cast<const mx_f4 *>(w + row);
-      const mx_i4 pv = *reinterpret_cast<const mx_i4 *>(p + row);
-      mx_u4 k;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) k[e] = rank_key(wv[e], pv[e], old);
-      return k;
-    };
-    auto counts_of = [&](int row, mx_u4 k) __attribute__((always_inline)) {  // above | equal << 16
-      int c = 0;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) c += row + e < n ? k[e] > prefix ? 1 : k[e] == prefix ? 1 << 16 : 0 : 0;
-      return c;
+      else return keys_of(row, *reinterpret_cast<const mx_f4 *>(w + row), *reinterpret_cast<const mx_i4 *>(p + row));
     };
     int above = 0, equal = 0;
 #pragma unroll 1
-    for (int row = r0 + 4 * lane; row < r1; row += 256) {
-      const int c = counts_of(row, keys_at(row));
-      above += c & 0xffff;
-      equal += c >> 16;
+    for (int r = r0; r < r1; r += 256) {
+      const mx_u4 k = keys_at(r + 4 * lane);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        above += __popcll(__ballot(k[e] > thr));
+        if (ties) equal += __popcll(__ballot(k[e] == prefix));
+      }
     }
-    for (int off = 32; off > 0; off >>= 1) above += __shfl_xor(above, off), equal += __shfl_xor(equal, off);
     if (lane == 0) red[wave][0] = above, red[wave][1] = equal;
     __syncthreads();
     above = equal = 0;  // before this wavefront's rows
 #pragma unroll
     for (int x = 0; x < SEL / 64; ++x) above += x < wave ? red[x][0] : 0, equal += x < wave ? red[x][1] : 0;
-    int *const holes = a.holes + head * a.half, *const movers = a.movers + head * a.half;
+    int *const holes = a.holes + head * a.half, *const movers = a.movers + head * a.half;  // (movers: counted from the last kept row, filled backwards)
 #pragma unroll 1
     for (int r = r0; r < r1; r += 256) {
       const int row = r + 4 * lane;
-      mx_u4 k = {0u, 0u, 0u, 0u};
-      mx_f4 wv = {0.f, 0.f, 0.f, 0.f};
-      mx_i4 pv = {0, 0, 0, 0};
-      if (row < n) k = keys_at(row);
-      if (apart && row < a.budget) {
-        wv = *reinterpret_cast<const mx_f4 *>(w + row);
-        pv = *reinterpret_cast<const mx_i4 *>(p + row);
+      const mx_u4 k = keys_at(row);
+      int mine = 0;  // above | equal << 16
+#pragma unroll
+      for (int e = 0; e < 4; ++e) mine += k[e] > thr ? 1 : 0;
+      if (ties) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mine += k[e] == prefix ? 1 << 16 : 0;
       }
-      const int mine = row < n ? counts_of(row, k) : 0, upto = wave_scan(mine), all = __builtin_amdgcn_readlane(upto, 63);
-      int sa = above + ((upto - mine) & 0xffff), se = equal + ((upto - mine) >> 16);
+      const int upto = wave_scan(mine), all = __builtin_amdgcn_readlane(upto, 63);
+      int sa = above + ((upto - mine) & 0xffff), se = equal + ((upto - mine) >> 16);  // rows before this lane's
       above += all & 0xffff;
       equal += all >> 16;
+      if (!ties && r >= a.budget) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int i = row + e, kept = sa + min(se, want);  // rows before i that stay
-        const bool is_above = i < n && k[e] > prefix, is_equal = i < n && k[e] == prefix, keep = is_above || (is_equal && se < want);
-        if (i < a.budget) {
-          if (!keep) holes[i - kept] = i;
-          else if (apart) wo[i] = wv[e], po[i] = pv[e];
-        } else if (keep) {
-          movers[a.budget - 1 - kept] = i;  // counted from the last kept row: the list is filled backwards
+        for (int e = 0; e < 4; ++e)
+          if (k[e] > thr) movers[(uint32_t)(a.budget - 1 - sa++)] = row + e;
+      } else if (!ties && r + 256 < a.budget) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (k[e] <= thr) holes[(uint32_t)(row + e - sa)] = row + e;
+          else ++sa;
         }
-        if (i == a.budget - 1) a.counts[head * 2] = a.budget - (kept + (keep ? 1 : 0));
-        sa += is_above;
-        se += is_equal;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int i = row + e, kept = sa + min(se, want);  // rows before i that stay
+          const bool is_above = k[e] > thr, is_equal = ties && k[e] == prefix, keep = is_above || (is_equal && se < want);
+          if (i < a.budget) {
+            if (!keep) holes[i - kept] = i;
+          } else if (keep && i < n) {
+            movers[a.budget - 1 - kept] = i;
+          }
+          if (i == a.budget - 1) a.counts[head * 2] = a.budget - (kept + (keep ? 1 : 0));
+          sa += is_above;
+          se += is_equal;
+        }
+      }
+    }
+    // Elsewhere the rows below `budget` go as they are, the holes too: the second launch fills those.  (In a loop of its own: with these loads
+    // in the one above, each of its turns waited for the last one's stores, which took 9 of 24 us on 32000 rows.)
+    if (apart) {
+#pragma unroll 4
+      for (int row = 4 * tid; row < a.budget; row += 4 * SEL) {
+        const mx_f4 wv = *reinterpret_cast<const mx_f4 *>(w + row);
+        const mx_i4 pv = *reinterpret_cast<const mx_i4 *>(p + row);
+        if (row + 4 <= a.budget) {
+          *reinterpret_cast<mx_f4 *>(wo + row) = wv;
+          *reinterpret_cast<mx_i4 *>(po + row) = pv;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 3; ++e)
+            if (row + e < a.budget) wo[row + e] = wv[e], po[row + e] = pv[e];
+        }
       }
     }
   }
