@@ -294,6 +294,38 @@ def test_evict(i, in_place):
                 assert (wo[b, g, m:] == 9).all() and (po[b, g, m:] == 9).all()
 
 
+@pytest.mark.parametrize("n,budget,recent", [(6, 3, 0), (37, 20, 5), (1001, 257, 0), (1030, 256, 100), (4099, 4097, 33), (33001, 9000, 7)])
+@pytest.mark.parametrize("kind", ["nan", "equal", "half nan", "newest many times", "extreme positions", "negative"])
+def test_evict_ties(kind, n, budget, recent):
+    """Ends inside a group of four rows, in a capacity whose rows behind the end would rank first; one output in place, the other not."""
+    T = -(-n // 32) * 32 + 64
+    say("case ties", kind, n, budget, recent)
+    cfg = config(1, T, 1, 1, 32)
+    cache = P.CCAMXCache.allocate(cfg, "cuda")
+    rng = np.random.default_rng(n)
+    w, p = np.full(T, np.inf, np.float32), np.full(T, 2 ** 31 - 1, np.int32)
+    p[:n] = rng.permutation(n)
+    w[:n] = {"nan": np.nan, "equal": 0.25}.get(kind, 1.0)
+    if kind == "half nan":
+        w[:n][rng.random(n) < 0.5] = np.nan
+    if kind == "newest many times":
+        p[:n] = np.where(rng.random(n) < 0.9, n, p[:n])
+        w[:n] = rng.random(n)
+    if kind == "extreme positions":
+        p[:n] = np.where(rng.random(n) < 0.5, -2 ** 31, 2 ** 31 - 1 - p[:n])
+        w[:n] = rng.integers(0, 3, n)
+    if kind == "negative":
+        w[:n] = -rng.integers(0, 4, n).astype(np.float32)
+    cache.weight.copy_(torch.from_numpy(w))
+    cache.pos.copy_(torch.from_numpy(p))
+    po = torch.full_like(cache.pos, 9)
+    P.cca_cache_evict_mx(cfg, cache, i32([n]), T, budget, recent, pos_out=po)
+    src = X.evict(w, p, n, budget, recent)
+    assert np.array_equal(cache.weight[0, 0, :budget].cpu().numpy(), w[src], equal_nan=True)
+    assert np.array_equal(po[0, 0, :budget].cpu().numpy(), p[src]) and (po[0, 0, budget:] == 9).all()
+    assert np.array_equal(cache.pos[0, 0].cpu().numpy(), p)
+
+
 def test_evict_ranks_by_position_then_weight_then_row():
     cfg = config(2, 64, 1, 1, 32)
     cache, _ = random_cache(cfg, 1)
