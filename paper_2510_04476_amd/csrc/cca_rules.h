@@ -470,7 +470,8 @@ constexpr size_t DECODE_UP_LDS = decode_up_lds(1, UP_CHANNELS);
 // without rows: 11.5, 11.8, 10.6, 10.7.
 // A head of few rounds goes to one workgroup - of eight wavefronts where that leaves CUs idle - which writes the result and adds up the
 // weights itself.  Without weights 1 x 1000: 7.8 us either way, a launch less for the host; 48 x 300, 8 x 32: 5.5, split 9.2.  With them, of
-// 6 sequences, 8 / 2 x 128: 500 rows 6.8, split 8.1; 1000 rows 9.1, 8.2; 16 / 1 x 64, 1000 rows 10.3, 12.3.
+// 6 sequences, 8 / 2 x 128: 500 rows 6.8, split 8.1; 1000 rows 9.1, 8.2; 16 / 1 x 64, 1000 rows 10.3, 12.3; where a
+// workgroup takes a whole long head, 128 sequences of 8192, 16 / 4 x 128: 145, by a second launch 151.
 struct MxSplit {
   int n, rows;  // splits, rows of each
   bool many;    // 8 wavefronts to a workgroup, else 4
