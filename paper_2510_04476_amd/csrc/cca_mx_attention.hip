@@ -517,6 +517,10 @@ hipError_t launch_width(int n32, const AttnArgs &a, bool many, hipStream_t s) {
   }
 }
 
+// Passes over a group's query heads, and the columns of one
+int columns(const Dims &d) { return d.bf16 && d.R <= 8 ? 8 : 16; }
+long long pass_groups(const Dims &d) { return (long long)d.B * d.Hk * ((d.R + columns(d) - 1) / columns(d)); }
+
 struct Layout {
   size_t state, part, scores, total;
 };
@@ -524,7 +528,7 @@ Layout layout(const Dims &d) {
   Layout L;
   size_t off = 0;
   auto take = [&](size_t n) { const size_t at = off; off += align256(n); return at; };
-  const size_t splits = (size_t)d.B * d.Hq * mx_max_splits((long long)d.B * d.Hk, d.T);
+  const size_t splits = (size_t)d.B * d.Hq * mx_max_splits(pass_groups(d), d.T);
   L.state = take(splits * sizeof(mx_f2));
   L.part = take(splits * d.dh * sizeof(float));
   L.scores = take((size_t)d.B * d.Hq * d.T * sizeof(float));
@@ -542,8 +546,8 @@ hipError_t mx_attention(const Dims &d, const cca_mx_cache &c, const void *q, boo
   unsigned char *ws = static_cast<unsigned char *>(workspace);
   const int longest = max_len + extra;
   const long long groups = (long long)d.B * d.Hk;
-  const int terms = !d.bf16 ? 3 : d.R <= 8 ? 1 : 2, cols = terms == 1 ? 8 : 16, passes = (d.R + cols - 1) / cols;
-  const MxSplit split = mx_split(groups * passes, d.T, longest, d.dh);
+  const int terms = !d.bf16 ? 3 : columns(d) == 8 ? 1 : 2, passes = (int)(pass_groups(d) / groups);
+  const MxSplit split = mx_split(pass_groups(d), longest, d.dh);
   const bool finish = split.n > 1 || (weight_out && passes > 1);
   auto p = [](const void *x) { return static_cast<const unsigned char *>(x); };
   AttnArgs a{d.B, d.T, d.Hq, d.Hk, d.R, max_len, extra, passes, split.n, split.rows, d.scale * 1.44269504088896340736f, len, q, q_f32 || !d.bf16,

@@ -476,16 +476,20 @@ struct MxSplit {
   int n, rows;  // splits, rows of each
   bool many;    // 8 wavefronts to a workgroup, else 4
 };
-constexpr int MX_MAX_SPLITS = 256;
+// Above 128 groups that is one split.  Where the groups then keep less than 65 % of the CUs busy (129 ... 166, 257 ... 332) long heads are taken in 8:
+// whole, 3, 8 splits, 8 / 2 x 128 of 16384 rows: 70 sequences 85, 69, 70, 150 150, 133, 135, with weights 225, 190, 182; 40, 16 / 4: 81, 75, 75; of
+// 4096 rows 150 41, 43, 44; with 75 % busy (96 sequences) 87, 98, 87.
+constexpr int MX_MAX_SPLITS = 256, MX_UNEVEN_ROWS = 8192;
+inline bool mx_uneven(long long groups) { return groups > 128 && groups * 100 < (groups + 255) / 256 * 256 * 65; }
 inline int mx_max_splits(long long groups, int T) {
-  const long long want = groups < 256 ? 256 / groups : 1, rounds = (T + 63) / 64;
+  const long long want = mx_uneven(groups) && T >= MX_UNEVEN_ROWS ? 8 : groups < 256 ? 256 / groups : 1, rounds = (T + 63) / 64;
   const long long s = want < rounds ? want : rounds;
   return (int)(s < MX_MAX_SPLITS ? s : MX_MAX_SPLITS);
 }
-inline MxSplit mx_split(long long groups, int T, int longest, int dh) {
+inline MxSplit mx_split(long long groups, int longest, int dh) {
   const int round = dh <= 128 ? 256 : 128;  // rows of four wavefronts at a time
   if (longest <= (groups <= 256 ? 4 : 2) * round) return {1, longest > 0 ? longest : 1, groups <= 256 && longest > round};
-  const int most = mx_max_splits(groups, T), even = (longest + most - 1) / most;
+  const int most = mx_max_splits(groups, longest), even = (longest + most - 1) / most;
   const int rows = (even > 0 ? (even + 127) / 128 : 1) * 128;  // (multiples of 64, 128 or 256: within 3 %)
   return {longest > rows ? (longest + rows - 1) / rows : 1, rows, dh > 128};
 }

@@ -9,8 +9,8 @@ SOURCE = r"""
 #include "cca_rules.h"
 extern "C" {
 int r_max_splits(long long groups, int T) { return cca::mx_max_splits(groups, T); }
-void r_split(long long groups, int T, int longest, int dh, int *out) {
-  const cca::MxSplit s = cca::mx_split(groups, T, longest, dh);
+void r_split(long long groups, int longest, int dh, int *out) {
+  const cca::MxSplit s = cca::mx_split(groups, longest, dh);
   out[0] = s.n, out[1] = s.rows, out[2] = s.many;
 }
 }
@@ -27,8 +27,8 @@ def max_splits(groups, T):
     return _lib.r_max_splits(C.c_longlong(groups), T)
 
 
-def split(groups, T, longest, dh):
+def split(groups, longest, dh):
     """(splits, rows of each, whether a workgroup has many wavefronts)"""
     out = (C.c_int * 3)()
-    _lib.r_split(C.c_longlong(groups), T, longest, dh, out)
+    _lib.r_split(C.c_longlong(groups), longest, dh, out)
     return out[0], out[1], bool(out[2])

@@ -182,12 +182,12 @@ def test_format_of_the_oracle():
     assert np.isnan(v[:2]).all() and np.isfinite(v[2]).all() and np.abs(v[2]).max() <= 6 * 2.0 ** 125
 
 
-@pytest.mark.parametrize("groups", [1, 2, 3, 16, 64, 300, 1024, 5000])
+@pytest.mark.parametrize("groups", [1, 2, 3, 16, 64, 128, 129, 160, 192, 300, 400, 1024, 5000])
 def test_splits_fit_the_workspace_and_whole_rounds(groups):
     for T in (32, 64, 320, 1024, 8192, 100000, 1 << 22):
         for dh in (32, 64, 96, 128, 160, 256):
             for longest in {1, 2, T // 3 + 1, T - 1, T}:
-                n, rows, _ = rules_mx.split(groups, T, longest, dh)
+                n, rows, _ = rules_mx.split(groups, longest, dh)
                 assert 1 <= n <= rules_mx.max_splits(groups, T) <= 256 and rows > 0
                 assert -(-longest // rows) == n and (n == 1 or rows % (64 if dh <= 128 else 32) == 0)
 
@@ -256,3 +256,9 @@ def test_batches_beyond_a_launch_are_refused():
     assert step() == B.CCA_ERR_SHAPE
     cfg.B = 65536
     assert step() == B.CCA_ERR_WORKSPACE
+
+
+def test_long_heads_that_leave_the_chip_unevenly_loaded_are_split():
+    split = lambda *a: rules_mx.split(*a)[0]
+    assert split(128, 16384, 128) == 2 and split(192, 16384, 128) == split(256, 16384, 128) == split(400, 16384, 128) == 1
+    assert split(150, 16384, 128) == split(300, 16384, 128) == 8 and split(150, 4096, 128) == split(300, 8191, 128) == 1
