@@ -468,6 +468,9 @@ constexpr size_t DECODE_UP_LDS = decode_up_lds(1, UP_CHANNELS);
 // rows, heads): 32 x 16384, 8 / 2 x 128: 29.2, 30.2, 31.9, 31.0; 16 x 16384: 17.6, 19.2; 48 x 8000, 4 / 1: 16.3, 18.0; 100 x 2000: 13.5,
 // 20.9; 20 x 3000, 4 / 4 x 256: 21.3, 20.3, of eight wavefronts 20.2; 7 x 9000: 19.3, 19.0, 18.9; 13 x 5003 of mixed lengths, 16 / 4 x 64, half of its workgroups
 // without rows: 11.5, 11.8, 10.6, 10.7.
+// Up to d_h = 96 a block is 6.5 KB or less; where there is at most a workgroup to a CU and it streams for long, its eight wavefronts ask for enough and four do not: 128 x 8192,
+// 8 / 2 x 64: 30.1, four 35.1; 20 x 30000, 16 / 4 x 64: 44.2, 49.5; 32 x 16384, 8 / 2 x 32: 17.1, 18.3, x 96: 24.6, 25.4, but x 128: 29.4, 28.3; 32 x 2048 (splits
+// of 1024): 13.0 both; 16 x 3000 (256): 8.6, 8.3; 300 x 900: 11.0, 10.4; 48 x 1024, 16 / 16: 14.8, 13.2.
 // A head of few rounds goes to one workgroup - of eight wavefronts where that leaves CUs idle - which writes the result and adds up the
 // weights itself.  Without weights 1 x 1000: 7.8 us either way, a launch less for the host; 48 x 300, 8 x 32: 5.5, split 9.2.  With them, of
 // 6 sequences, 8 / 2 x 128: 500 rows 6.8, split 8.1; 1000 rows 9.1, 8.2; 16 / 1 x 64, 1000 rows 10.3, 12.3; where a
@@ -479,7 +482,7 @@ struct MxSplit {
 // Above 128 groups that is one split.  Where the groups then keep less than 65 % of the CUs busy (129 ... 166, 257 ... 332) long heads are taken in 8:
 // whole, 3, 8 splits, 8 / 2 x 128 of 16384 rows: 70 sequences 85, 69, 70, 150 150, 133, 135, with weights 225, 190, 182; 40, 16 / 4: 81, 75, 75; of
 // 4096 rows 150 41, 43, 44; with 75 % busy (96 sequences) 87, 98, 87.
-constexpr int MX_MAX_SPLITS = 256, MX_UNEVEN_ROWS = 8192;
+constexpr int MX_MAX_SPLITS = 256, MX_UNEVEN_ROWS = 8192, MX_EIGHT_ROWS = 1536;
 inline bool mx_uneven(long long groups) { return groups > 128 && groups * 100 < (groups + 255) / 256 * 256 * 65; }
 inline int mx_max_splits(long long groups, int T) {
   const long long want = mx_uneven(groups) && T >= MX_UNEVEN_ROWS ? 8 : groups < 256 ? 256 / groups : 1, rounds = (T + 63) / 64;
@@ -491,7 +494,7 @@ inline MxSplit mx_split(long long groups, int longest, int dh) {
   if (longest <= (groups <= 256 ? 4 : 2) * round) return {1, longest > 0 ? longest : 1, groups <= 256 && longest > round};
   const int most = mx_max_splits(groups, longest), even = (longest + most - 1) / most;
   const int rows = (even > 0 ? (even + 127) / 128 : 1) * 128;  // (multiples of 64, 128 or 256: within 3 %)
-  return {longest > rows ? (longest + rows - 1) / rows : 1, rows, dh > 128};
+  return {longest > rows ? (longest + rows - 1) / rows : 1, rows, dh > 128 || (dh <= 96 && groups <= 256 && rows >= MX_EIGHT_ROWS)};
 }
 
 // ---- projections with 4-bit weights: rows of x to a workgroup, 16 or 32 columns ---------------------------------------------

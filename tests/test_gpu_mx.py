@@ -133,15 +133,17 @@ def test_attention_with_more_heads_than_a_pass_takes(Bn, T, Hq, Hk, dh, dt):
     assert (o == 0).all() and torch.isneginf(lse).all() and torch.equal(cache.weight, before)
 
 
-def test_attention_of_many_long_heads():
-    """150 groups of up to 8224 rows: eight splits to a head, most sequences short of some of them."""
-    cfg = config(150, 8224, 2, 1, 32)
-    lens = np.random.default_rng(2).integers(0, 8225, 150)
-    lens[:3] = 0, 8224, 1
+@pytest.mark.parametrize("Bn,T,dh", [(150, 8224, 32), (128, 3232, 96), (200, 1632, 64)])
+def test_attention_of_many_long_heads(Bn, T, dh):
+    """Eight splits to a head, most sequences short of some of them; two of eight wavefronts; one of eight, which adds up the weights."""
+    say("case many", Bn, T, dh)
+    cfg = config(Bn, T, 2, 1, dh)
+    lens = np.random.default_rng(2).integers(0, T + 1, Bn)
+    lens[:3] = 0, T, 1
     cache, vals = random_cache(cfg, 12, lens)
-    q = rounded(np.random.default_rng(13).standard_normal((150, 2, 32)), "bf16").cuda()
+    q = rounded(np.random.default_rng(13).standard_normal((Bn, 2, dh)), "bf16").cuda()
     before = cache.weight.clone()
-    o, lse = P.cca_decode_attention_mx(cfg, cache, q, i32(lens), 8224, want_lse=True, weight_in=before, weight_out=cache.weight)
+    o, lse = P.cca_decode_attention_mx(cfg, cache, q, i32(lens), T, want_lse=True, weight_in=before, weight_out=cache.weight)
     torch.cuda.synchronize()
     check_attention(cfg, vals, q, lens, o, lse, cache.weight, before, before)
 

@@ -262,3 +262,11 @@ def test_long_heads_that_leave_the_chip_unevenly_loaded_are_split():
     split = lambda *a: rules_mx.split(*a)[0]
     assert split(128, 16384, 128) == 2 and split(192, 16384, 128) == split(256, 16384, 128) == split(400, 16384, 128) == 1
     assert split(150, 16384, 128) == split(300, 16384, 128) == 8 and split(150, 4096, 128) == split(300, 8191, 128) == 1
+
+
+def test_wavefronts_of_a_split():
+    many = lambda *a: rules_mx.split(*a)[2]
+    assert many(8, 9000, 256) and many(128, 8192, 64) and many(64, 16384, 96) and many(64, 16384, 32)
+    assert not (many(64, 16384, 128) or many(300, 9000, 64) or many(64, 4096, 64) or many(16, 3000, 64))
+    # one workgroup to a head
+    assert many(2, 1000, 128) and not many(2, 200, 128) and not many(300, 500, 128)
