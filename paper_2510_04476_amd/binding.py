@@ -514,7 +514,7 @@ def cca_decode_step_static(cfg: CCAConfig, w: CCAWeights, x_new, state: CCADecod
 # ---- serving with 4 bits a number (format and layouts: cca.h) --------------
 # A call of these takes a few microseconds on the GPU, so what Python spends on one counts: plain comparisons, the config's C form kept
 # until a field changes, the current stream's handle without a Stream object around it.
-_raw_stream = torch._C._cuda_getCurrentRawStream
+_raw_stream, _current = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
 def _mx_ptr(name, t, shape, dtype, index):
@@ -548,7 +548,7 @@ def _mx_call(where, index, *args):
     if index < 0:
         raise ValueError(f"{where}: tensors on the CPU, expected a GPU")
     fn = getattr(_lib or load_library(), where)
-    if index == torch._C._cuda_getDevice():
+    if index == _current():
         status = fn(*args, _raw_stream(index))
     else:
         with torch.cuda.device(index):
@@ -657,10 +657,11 @@ def cca_project_mx(x: torch.Tensor, w: CCAMXWeight, out: torch.Tensor | None = N
     dt, shape, index = x.dtype, x.shape, w._index
     if (dt is not torch.bfloat16 and dt is not torch.float32) or not shape or shape[-1] != w.K:
         raise ValueError(f"cca_project_mx: x {dt} {tuple(shape)}, weight of K = {w.K}")
-    y_shape = (*shape[:-1], w.N)
-    x_ptr = _mx_ptr("x", x, shape, dt, index)
+    K, N = w.K, w.N
+    y_shape = (shape[0], N) if len(shape) == 2 else (*shape[:-1], N)
+    x_ptr = x.data_ptr() if x.get_device() == index and x.is_contiguous() else _mx_ptr("x", x, shape, dt, index)
     out, out_ptr = _mx_out("out", out, y_shape, dt, index, x)
-    _mx_call("cca_project_mx", index, x_ptr, w.ref(), out_ptr, x.numel() // w.K, w.K, w.N, CCA_BF16 if dt is torch.bfloat16 else CCA_F32)
+    _mx_call("cca_project_mx", index, x_ptr, w.ref(), out_ptr, x.numel() // K, K, N, CCA_BF16 if dt is torch.bfloat16 else CCA_F32)
     return out
 
 
@@ -671,8 +672,8 @@ def cca_cache_append_mx(cfg: CCAConfig, cache: CCAMXCache, k, v, rows, pos=None,
     n = k.shape[1] if k.dim() == 4 else 0
     shape = (cfg.B, n, cfg.n_kv_heads, cfg.head_dim)
     _mx_call("cca_cache_append_mx", index, cfg.ref(), cache._for(cfg), _mx_ptr("k", k, shape, dt, index), _mx_ptr("v", v, shape, dt, index), n,
-             _mx_ptr("rows", rows, per_seq, torch.int32, index), _mx_opt("counts", counts, per_seq, torch.int32, index),
-             _mx_opt("pos", pos, per_seq, torch.int32, index))
+             _mx_ptr("rows", rows, per_seq, torch.int32, index), None if counts is None else _mx_ptr("counts", counts, per_seq, torch.int32, index),
+             None if pos is None else _mx_ptr("pos", pos, per_seq, torch.int32, index))
 
 
 def cca_cache_rows_mx(cfg: CCAConfig, cache: CCAMXCache, n: int, first=None, count=None, k=None, v=None):
@@ -680,9 +681,14 @@ def cca_cache_rows_mx(cfg: CCAConfig, cache: CCAMXCache, n: int, first=None, cou
     index, dt, per_seq = cache._index, cfg.torch_dtype, (cfg.B,)
     shape = (cfg.B, n, cfg.n_kv_heads, cfg.head_dim)
     k, k_ptr = _mx_out("k", k, shape, dt, index, cache.k_codes)
-    v, v_ptr = _mx_out("v", v, shape, dt, index, cache.k_codes)
+    if v is None:
+        v = torch.empty_like(k)
+        v_ptr = v.data_ptr()
+    else:
+        v_ptr = _mx_ptr("v", v, shape, dt, index)
     _mx_call("cca_cache_rows_mx", index, cfg.ref(), cache._for(cfg), k_ptr, v_ptr, n,
-             _mx_opt("first", first, per_seq, torch.int32, index), _mx_opt("count", count, per_seq, torch.int32, index))
+             None if first is None else _mx_ptr("first", first, per_seq, torch.int32, index),
+             None if count is None else _mx_ptr("count", count, per_seq, torch.int32, index))
     return k, v
 
 
@@ -697,11 +703,13 @@ def cca_decode_attention_mx(cfg: CCAConfig, cache: CCAMXCache, q, lens, max_len:
         lse, lse_ptr = _mx_out("lse", lse, (B, Hq), torch.float32, index, cache.k_codes)
     if workspace is None:
         workspace = new_mx_workspace(cfg, cache._device)
-    w = (B, cfg.n_kv_heads, cfg.T)
+    in_ptr = out_ptr = None
+    if weight_in is not None or weight_out is not None:
+        w = (B, cfg.n_kv_heads, cfg.T)
+        in_ptr, out_ptr = _mx_opt("weight_in", weight_in, w, torch.float32, index), _mx_opt("weight_out", weight_out, w, torch.float32, index)
     _mx_call("cca_decode_attention_mx", index, cfg.ref(), cache._for(cfg), _mx_ptr("q", q, (B, Hq, dh), dt, index),
-             _mx_ptr("lens", lens, (B,), torch.int32, index), max_len, o_ptr, lse_ptr, _mx_opt("weight_in", weight_in, w, torch.float32, index),
-             _mx_opt("weight_out", weight_out, w, torch.float32, index),
-             _mx_workspace(workspace, index), workspace.numel())
+             _mx_ptr("lens", lens, (B,), torch.int32, index), max_len, o_ptr, lse_ptr, in_ptr, out_ptr, _mx_workspace(workspace, index),
+             workspace.numel())
     return (o, lse) if want_lse else o
 
 
