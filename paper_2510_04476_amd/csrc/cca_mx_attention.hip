@@ -377,7 +377,7 @@ __global__ __launch_bounds__(WAVES * 64, (WAVES == 4 ? Form<N32, TERMS>::RESIDEN
 }
 
 // ---------------------------------------------------------------------------
-// What follows the splits, in one launch.  The first workgroups join them: o = sum o_s 2^(m_s - M) / sum l_s 2^(m_s - M), some channels
+// What follows the splits, in one launch.  Some workgroups join them: o = sum o_s 2^(m_s - M) / sum l_s 2^(m_s - M), some channels
 // of a query head each.  The others form the weights: weight_out[row] = weight_in[row] + sum over
 // the R query heads of 2^(score - M) / L, four rows a thread.  Bound by the scores, 4 R bytes a row beside 8 of the weights: 32 x 16384, 8 / 2: 8.5 us
 // for 25 MB; the join alone 3.3 us, a launch and two latencies.
@@ -418,7 +418,9 @@ __global__ __launch_bounds__(256) void mx_finish_kernel(AttnArgs a, int dh, unsi
   constexpr int PARTS = 256 / CH;
   __shared__ float f[256], acc[PARTS][CH], top[W_HEADS], inv[W_HEADS];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  for (unsigned item = blockIdx.x; item < items; item += gridDim.x, __syncthreads()) {
+  for (unsigned place = blockIdx.x; place < items; place += gridDim.x, __syncthreads()) {
+    // the longer items, those of the weights, come first
+    const unsigned item = place < items - joins ? place + joins : place - (items - joins);
     mx_f2 st[4];
     if (item < joins) {
       const unsigned chunks = (unsigned)(dh + CH - 1) / CH;
