@@ -569,3 +569,24 @@ def test_results_repeat_bit_for_bit():
         runs.append((*P.cca_decode_attention_mx(cfg, cache, q, i32(lens), 2048, want_lse=True, weight_out=w), w))
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for r in runs[1:] for a, b in zip(runs[0], r))
+
+
+def test_batches_with_more_heads_than_a_launch_has_workgroups():
+    """1.3 million heads (launches of at most 2^20 workgroups take the rest in turn; offsets pass 32 bits): two sequences again and again give
+    what the two alone give, bit for bit."""
+    def run(times):
+        cfg = P.CCAConfig(B=2 * times, T=32, d_model=2720, n_q_heads=85, n_kv_heads=5, head_dim=32)
+        g = torch.Generator(device="cuda").manual_seed(1)
+        draw = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16().repeat(times, *[1] * (len(s) - 1))
+        k, v, q = draw(2, 30, 5, 32), draw(2, 30, 5, 32), draw(2, 85, 32)
+        counts = i32([30, 21]).repeat(times)
+        cache, ws = P.CCAMXCache.allocate(cfg, "cuda"), P.new_mx_workspace(cfg, "cuda")
+        P.cca_cache_append_mx(cfg, cache, k, v, torch.zeros_like(counts), counts=counts)
+        o, lse = P.cca_decode_attention_mx(cfg, cache, q, counts, 32, want_lse=True, weight_in=cache.weight, weight_out=cache.weight, workspace=ws)
+        P.cca_cache_evict_mx(cfg, cache, counts, 32, 11, 3, workspace=ws)
+        out = (o, lse, cache.weight[..., :11], cache.pos[..., :11], counts, *P.cca_cache_rows_mx(cfg, cache, 11))
+        torch.cuda.synchronize()
+        return [x.reshape(times, 2, *x.shape[1:]) for x in out]
+
+    for one, many in zip(run(1), run(1 << 17)):
+        assert (many == one).all()
